@@ -81,7 +81,8 @@ typedef enum {
   SLA_ERR_HIP = -7,         /* a kernel launch reported an error */
   SLA_ERR_LAYOUT = -8,      /* strides negative, not multiples of 8 elements, token stride < d, or a
                                base pointer not 16-byte aligned */
-  SLA_ERR_STATIC_LIMIT = -9 /* sla_classify_blocks_static: the problem needs more than SLA_STATIC_SCRATCH_BYTES */
+  SLA_ERR_STATIC_LIMIT = -9, /* sla_classify_blocks_static: the problem needs more than SLA_STATIC_SCRATCH_BYTES */
+  SLA_ERR_VALUE = -10       /* a scalar out of its range: eps, theta or scale of rope.h, norm.h, w8a8.h, xattn.h */
 } sla_status;
 
 typedef enum { SLA_PHI_SOFTMAX = 0, SLA_PHI_ELU1 = 1, SLA_PHI_RELU = 2 } sla_phi;

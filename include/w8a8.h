@@ -79,6 +79,29 @@ int w8a8_quantize_act(const void* x, int M, int K, void* workspace, size_t works
 int w8a8_gemm_fwd(const void* workspace, size_t workspace_bytes, const void* wq, const void* bias,
                   void* y, int M, int N, int K, sla_stream_t stream);
 
+/* ---- The norm in front of the layer ----
+ *
+ * y = W8A8-linear(n) with n the root-mean-square norm of the residual stream (norm.h):
+ *   h = x + res, rounded to bf16 (without res: h = x),   n = h r o norm_w,
+ *   r = 1 / sqrt(mean(h^2) + eps) over the K features.
+ * n goes from fp32 straight to its INT8 codes (the block scales are those of n, not of a bf16 copy of it),
+ * and is never written; h is, for whoever reads the stream next.
+ *   x       in   bf16 [M, K]
+ *   res     in   bf16 [M, K]; NULL = none (then h is NULL too, else SLA_ERR_NULL)
+ *   norm_w  in   bf16 [K]; NULL = ones
+ *   h       out  bf16 [M, K]
+ * All of them 16-byte aligned (else SLA_ERR_LAYOUT); K <= 16384 here; eps > 0 (else SLA_ERR_VALUE).
+ * The workspace of w8a8_norm_workspace_bytes(M, K) bytes holds the quantised activations and the rows'
+ * factors; behind w8a8_norm_quantize_act it is one that w8a8_gemm_fwd takes for the same M and K.
+ * Values are expected finite, and the mean of a row's squares within fp32 (|h| below 1e19); others make that row
+ * NaN or zero, and a NaN has no code: it is undefined which of its block's codes change. */
+size_t w8a8_norm_workspace_bytes(int M, int K);
+int w8a8_norm_quantize_act(const void* x, const void* res, const void* norm_w, void* h, int M, int K, double eps,
+                           void* workspace, size_t workspace_bytes, sla_stream_t stream);
+int w8a8_norm_linear_fwd(const void* x, const void* res, const void* norm_w, void* h, const void* wq, const void* bias,
+                         void* y, int M, int N, int K, double eps, void* workspace, size_t workspace_bytes,
+                         sla_stream_t stream);
+
 /* For tests: the codes and scales held by a weight object (R = N) or by a workspace filled
  * for R = M tokens, in plain layouts: codes int8 [R, K] row-major, scales fp32
  * [ceil(R / 128), K / 128] row-major.  Either output may be NULL.

@@ -1,7 +1,7 @@
 """ctypes binding of libsla.so: argument marshalling only.
 
 Every function here has the name and the argument order of the C entry point
-it calls (include/sla.h); tensors are PyTorch CUDA tensors used purely as
+it calls (include/*.h); tensors are PyTorch CUDA tensors used purely as
 device memory, the stream is PyTorch's current stream.  No step of the path
 runs in Python, and there is no fallback: if the library is missing or a call
 returns an error status, an exception is raised.
@@ -23,6 +23,7 @@ SLA_OK = 0
 ERR_NULL, ERR_SHAPE, ERR_BLOCK, ERR_RATIO, ERR_WORKSPACE, ERR_UNSUPPORTED, ERR_HIP = -1, -2, -3, -4, -5, -6, -7
 ERR_LAYOUT = -8
 ERR_STATIC_LIMIT = -9
+ERR_VALUE = -10
 STATIC_SCRATCH_BYTES = 64 << 20
 
 EXPORTS = ("sla_version", "sla_status_string", "sla_block_counts", "sla_workspace_bytes",
@@ -31,7 +32,10 @@ EXPORTS = ("sla_version", "sla_status_string", "sla_block_counts", "sla_workspac
            "sla_linear_attn_fwd", "sla_debug_e4m3_encode", "sla_debug_quantize_kv", "sla_debug_quantize_q", "sla_calibrate_mfma",
            "sla_profile_enable", "sla_profile_reset", "sla_profile_read")
 W8A8_EXPORTS = ("w8a8_weight_bytes", "w8a8_quantize_weight", "w8a8_workspace_bytes", "w8a8_linear_fwd",
-                "w8a8_quantize_act", "w8a8_gemm_fwd", "w8a8_debug_unpack")
+                "w8a8_quantize_act", "w8a8_gemm_fwd", "w8a8_debug_unpack", "w8a8_norm_workspace_bytes",
+                "w8a8_norm_quantize_act", "w8a8_norm_linear_fwd")
+ROPE_EXPORTS = ("rope_make_plan", "rope_qk_fwd", "rope_bwd_workspace_bytes", "rope_qk_bwd")
+NORM_EXPORTS = ("norm_rms_fwd", "norm_bwd_workspace_bytes", "norm_rms_bwd")
 BWD_EXPORTS = ("sla_bwd_workspace_bytes", "sla_attention_bwd", "sla_saved_bytes", "sla_attention_fwd_train",
                "sla_attention_bwd_saved", "sla_attention_fwd_train_strided", "sla_attention_bwd_strided")
 N_STAGES = 5
@@ -48,6 +52,17 @@ class Strides(ctypes.Structure):
 class BwdStrides(ctypes.Structure):
     """sla_bwd_strides of include/sla_bwd.h: one layout (or NULL = contiguous) per tensor."""
     _fields_ = [(n, ctypes.POINTER(Strides)) for n in ("q", "k", "v", "dout", "dq", "dk", "dv")]
+
+
+class RopePlan(ctypes.Structure):
+    """rope_plan of include/rope.h (made by rope_make_plan)."""
+    _fields_ = [("made", ctypes.c_int32), ("pairing", ctypes.c_int32), ("turns", ctypes.c_uint64 * 64),
+                ("axis", ctypes.c_uint8 * 64)]
+
+
+class RopeBwdStrides(ctypes.Structure):
+    """rope_bwd_strides of include/rope.h."""
+    _fields_ = [(n, ctypes.POINTER(Strides)) for n in ("dq_out", "dk_out", "q", "k", "dq", "dk")]
 
 
 class SLAError(RuntimeError):
@@ -141,6 +156,30 @@ def lib():
         L.w8a8_gemm_fwd.argtypes = [c_vp, c_sz, c_vp, c_vp, c_vp] + [c_int] * 3 + [c_vp]
         L.w8a8_debug_unpack.restype = c_int
         L.w8a8_debug_unpack.argtypes = [c_vp, c_int, c_int, c_int, c_vp, c_vp, c_vp]
+        L.w8a8_norm_workspace_bytes.restype = c_sz
+        L.w8a8_norm_workspace_bytes.argtypes = [c_int, c_int]
+        L.w8a8_norm_quantize_act.restype = c_int
+        L.w8a8_norm_quantize_act.argtypes = [c_vp] * 4 + [c_int] * 2 + [c_dbl, c_vp, c_sz, c_vp]
+        L.w8a8_norm_linear_fwd.restype = c_int
+        L.w8a8_norm_linear_fwd.argtypes = [c_vp] * 7 + [c_int] * 3 + [c_dbl, c_vp, c_sz, c_vp]
+        # include/rope.h
+        L.rope_make_plan.restype = c_int
+        L.rope_make_plan.argtypes = [ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(c_dbl), c_int, ctypes.POINTER(RopePlan)]
+        L.rope_qk_fwd.restype = c_int
+        L.rope_qk_fwd.argtypes = ([c_vp] * 4 + [sp] * 4 + [c_vp, ctypes.c_int64, c_vp, c_vp, c_int, c_dbl] + [c_int] * 5 +
+                                  [ctypes.POINTER(RopePlan), c_vp])
+        L.rope_bwd_workspace_bytes.restype = c_sz
+        L.rope_bwd_workspace_bytes.argtypes = [c_int] * 6
+        L.rope_qk_bwd.restype = c_int
+        L.rope_qk_bwd.argtypes = ([c_vp] * 8 + [ctypes.POINTER(RopeBwdStrides), c_vp, ctypes.c_int64, c_vp, c_vp, c_int, c_dbl] +
+                                  [c_int] * 5 + [ctypes.POINTER(RopePlan), c_vp, c_sz, c_vp])
+        # include/norm.h
+        L.norm_rms_fwd.restype = c_int
+        L.norm_rms_fwd.argtypes = [c_vp] * 5 + [c_int] * 2 + [c_dbl, c_vp]
+        L.norm_bwd_workspace_bytes.restype = c_sz
+        L.norm_bwd_workspace_bytes.argtypes = [c_int] * 2
+        L.norm_rms_bwd.restype = c_int
+        L.norm_rms_bwd.argtypes = [c_vp] * 6 + [c_int] * 2 + [c_dbl, c_vp, c_sz, c_vp]
         _lib = L
     return _lib
 
@@ -558,3 +597,225 @@ def sla_fwd_attend(q, out, block_q, block_k, topk_ratio, marginal_ratio, workspa
     st = lib().sla_fwd_attend(_ptr(q), _ptr(out), ctypes.byref(sq), ctypes.byref(so_), B, H, N, d, block_q, block_k,
                               topk_ratio, marginal_ratio, _ptr(proj_b), phi_kind, _ptr(workspace), workspace.numel(), _stream())
     _check(st, "sla_fwd_attend")
+
+
+# ---------------------------------------------------------------------------
+# include/rope.h, include/norm.h and the norm in front of a W8A8 layer
+# ---------------------------------------------------------------------------
+class _on:
+    """Makes the device of `t` the current one for a call, so that the launch and its stream are that device's; every
+    other tensor of the call has to lie there."""
+
+    def __init__(self, t, *others):
+        if not t.is_cuda:
+            raise ValueError("expected CUDA tensors")
+        for o in others:
+            if o is not None and o.device != t.device:
+                raise ValueError("the tensors of a call have to lie on one device")
+        self.other = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
+
+
+def _rows_of(t, what, shape=None):
+    """A contiguous CUDA bfloat16 matrix [M, K] (of that shape)."""
+    if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 2 or not t.is_contiguous() or (shape and tuple(t.shape) != shape):
+        raise ValueError("%s: expected a contiguous 2-D CUDA bfloat16 tensor%s" % (what, " of %r" % (shape,) if shape else ""))
+    return tuple(t.shape)
+
+
+def _vector(t, what, n, dtype=torch.bfloat16):
+    if t is not None and (t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() != n):
+        raise ValueError("%s: expected a contiguous CUDA %s tensor of %d elements" % (what, dtype, n))
+
+
+def _scratch(workspace, nbytes, device, where):
+    """The caller's workspace, or one of the size the library asks for."""
+    if workspace is None:
+        if nbytes == 0:
+            raise ValueError("unsupported problem for %s" % where)
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous uint8 tensor")
+    return workspace
+
+
+ROPE_PAIRINGS = {"interleaved": 0, "halves": 1}
+ROPE_NORMS = {"none": 0, "head": 1, "token": 2}
+
+
+def rope_make_plan(pairs=(22, 21, 21), theta=10000.0, pairing="interleaved"):
+    """How the 64 channel pairs of a head turn: pairs per axis (time, height, width), base of each axis (one number: of all),
+    "interleaved" (2 j, 2 j + 1) or "halves" (j, j + 64)."""
+    theta = (theta,) * 3 if isinstance(theta, (int, float)) else tuple(theta)
+    if len(pairs) != 3 or len(theta) != 3 or pairing not in ROPE_PAIRINGS:
+        raise ValueError("three axes, and pairing one of %s" % ", ".join(sorted(ROPE_PAIRINGS)))
+    plan = RopePlan()
+    _check(lib().rope_make_plan((ctypes.c_int32 * 3)(*pairs), (ctypes.c_double * 3)(*theta), ROPE_PAIRINGS[pairing],
+                                ctypes.byref(plan)), "rope_make_plan")
+    return plan
+
+
+def _rope_args(q, k, positions, norm, q_weight, k_weight):
+    """(B, H, Hk, N, d, int32 from one sample's positions to the next's, norm's number)"""
+    B, H, N, d = q.shape
+    Hk = 0
+    if k is not None:
+        if k.dim() != 4 or (k.shape[0], k.shape[2], k.shape[3]) != (B, N, d):
+            raise ValueError("q and k: one [B, heads, N, d], whose heads may differ")
+        Hk = k.shape[1]
+    if norm not in ROPE_NORMS:
+        raise ValueError("norm: one of %s" % ", ".join(sorted(ROPE_NORMS)))
+    if (positions.dtype != torch.int32 or not positions.is_cuda or not positions.is_contiguous() or
+            tuple(positions.shape) not in ((N, 3), (1, N, 3), (B, N, 3))):
+        raise ValueError("positions: expected a contiguous CUDA int32 tensor [N, 3] or [B, N, 3]")
+    if norm != "none":
+        _vector(q_weight, "q_weight", d if norm == "head" else H * d)
+        _vector(k_weight, "k_weight", d if norm == "head" else Hk * d)
+    return B, H, Hk, N, d, 3 * N if positions.dim() == 3 and positions.shape[0] > 1 else 0, ROPE_NORMS[norm]
+
+
+def _heads_like(x):
+    return torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
+
+
+def _strides_or_none(t, what, like):
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(like.shape):
+        raise ValueError("%s: expected the shape %r" % (what, tuple(like.shape)))
+    return ctypes.pointer(_strides_of(t, what))
+
+
+def rope_qk_fwd(q, k, positions, plan, q_weight=None, k_weight=None, norm="none", eps=1e-6, q_out=None, k_out=None):
+    """(q_out, k_out): q [B,H,N,d] and k [B,Hk,N,d] (or None), in any memory order with contiguous channels, normed
+    ("none", "head", "token") and turned by `positions` (int32 [N, 3] or [B, N, 3])."""
+    B, H, Hk, N, d, pb, kind = _rope_args(q, k, positions, norm, q_weight, k_weight)
+    q_out = _heads_like(q) if q_out is None else q_out
+    k_out = _heads_like(k) if k_out is None and k is not None else k_out
+    s = [_strides_or_none(t, n, like) for t, n, like in ((q, "q", q), (k, "k", k), (q_out, "q_out", q), (k_out, "k_out", k))]
+    with _on(q, k, q_out, k_out, positions, q_weight, k_weight):
+        st = lib().rope_qk_fwd(_ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), *s, _ptr(positions), pb, _ptr(q_weight),
+                               _ptr(k_weight), kind, eps, B, H, Hk, N, d, ctypes.byref(plan), _stream())
+    _check(st, "rope_qk_fwd")
+    return q_out, k_out
+
+
+def rope_bwd_workspace_bytes(B, H, Hk, N, d, norm):
+    return lib().rope_bwd_workspace_bytes(B, H, Hk, N, d, ROPE_NORMS[norm])
+
+
+def rope_qk_bwd(dq_out, dk_out, positions, plan, q=None, k=None, q_weight=None, k_weight=None, norm="none", eps=1e-6, dq=None,
+                dk=None, want_dw=True, workspace=None):
+    """(dq, dk, dq_weight or None, dk_weight or None) of rope_qk_fwd; q and k are the forward pass's inputs (needed with a
+    norm); the weights' gradients are fp32, and None without a norm or with want_dw False."""
+    B, H, Hk, N, d, pb, kind = _rope_args(dq_out, dk_out, positions, norm, q_weight, k_weight)
+    if norm == "none":
+        q = k = q_weight = k_weight = None
+    dq = _heads_like(dq_out) if dq is None else dq
+    dk = _heads_like(dk_out) if dk is None and dk_out is not None else dk
+    named = ((dq_out, "dq_out", dq_out), (dk_out, "dk_out", dk_out), (q, "q", dq_out), (k, "k", dk_out), (dq, "dq", dq_out),
+             (dk, "dk", dk_out))
+    s = RopeBwdStrides(*[_strides_or_none(*x) for x in named])
+    dqw = dkw = None
+    if want_dw and norm != "none":
+        dqw = torch.empty(d if norm == "head" else H * d, dtype=torch.float32, device=dq_out.device)
+        if dk_out is not None:
+            dkw = torch.empty(d if norm == "head" else Hk * d, dtype=torch.float32, device=dq_out.device)
+        workspace = _scratch(workspace, lib().rope_bwd_workspace_bytes(B, H, Hk, N, d, kind), dq_out.device, "rope_qk_bwd")
+    with _on(dq_out, dk_out, q, k, dq, dk, positions, q_weight, k_weight, workspace):
+        st = lib().rope_qk_bwd(_ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(dq), _ptr(dk), _ptr(dqw), _ptr(dkw),
+                               ctypes.byref(s), _ptr(positions), pb, _ptr(q_weight), _ptr(k_weight), kind, eps, B, H, Hk, N, d,
+                               ctypes.byref(plan), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
+    _check(st, "rope_qk_bwd")
+    return dq, dk, dqw, dkw
+
+
+def norm_rms_fwd(x, w, res=None, eps=1e-6, out=None, h=None):
+    """(y, h): h = x + res in bf16 (x itself without res), y its root-mean-square norm times w (None: ones)."""
+    M, K = _rows_of(x, "x")
+    _vector(w, "w", K)
+    out = torch.empty_like(x) if out is None else out
+    _rows_of(out, "out", (M, K))
+    if res is not None:
+        _rows_of(res, "res", (M, K))
+        h = torch.empty_like(x) if h is None else h
+        _rows_of(h, "h", (M, K))
+    elif h is not None:
+        raise ValueError("h is written only where there is a res")
+    with _on(x, w, res, out, h):
+        st = lib().norm_rms_fwd(_ptr(x), _ptr(res), _ptr(w), _ptr(h), _ptr(out), M, K, eps, _stream())
+    _check(st, "norm_rms_fwd")
+    return out, x if res is None else h
+
+
+def norm_bwd_workspace_bytes(M, K):
+    return lib().norm_bwd_workspace_bytes(M, K)
+
+
+def norm_rms_bwd(dy, h, w, dh=None, eps=1e-6, dx=None, want_dw=True, workspace=None):
+    """(dx, dw fp32 [K] or None) of norm_rms_fwd, h being the stored stream; dh: the gradient that h has from elsewhere."""
+    M, K = _rows_of(dy, "dy")
+    _rows_of(h, "h", (M, K))
+    _vector(w, "w", K)
+    if dh is not None:
+        _rows_of(dh, "dh", (M, K))
+    dx = torch.empty_like(dy) if dx is None else dx
+    _rows_of(dx, "dx", (M, K))
+    dw = None
+    if want_dw:
+        dw = torch.empty(K, dtype=torch.float32, device=dy.device)
+        workspace = _scratch(workspace, norm_bwd_workspace_bytes(M, K), dy.device, "norm_rms_bwd")
+    with _on(dy, h, w, dh, dx, workspace):
+        st = lib().norm_rms_bwd(_ptr(dy), _ptr(dh), _ptr(h), _ptr(w), _ptr(dx), _ptr(dw), M, K, eps, _ptr(workspace),
+                                0 if workspace is None else workspace.numel(), _stream())
+    _check(st, "norm_rms_bwd")
+    return dx, dw
+
+
+def w8a8_norm_workspace_bytes(M, K):
+    return lib().w8a8_norm_workspace_bytes(M, K)
+
+
+def _w8a8_norm_args(x, norm_w, res, h, workspace, where):
+    M, K = _rows_of(x, "x")
+    _vector(norm_w, "norm_w", K)
+    if res is not None:
+        _rows_of(res, "res", (M, K))
+        h = torch.empty_like(x) if h is None else h
+        _rows_of(h, "h", (M, K))
+    elif h is not None:
+        raise ValueError("h is written only where there is a res")
+    return M, K, h, _scratch(workspace, w8a8_norm_workspace_bytes(M, K), x.device, where)
+
+
+def w8a8_norm_quantize_act(x, norm_w, res=None, eps=1e-6, h=None, workspace=None):
+    """(workspace, h): a workspace for w8a8_gemm_fwd holding the quantised norm of h = x + res (x itself without res)."""
+    M, K, h, workspace = _w8a8_norm_args(x, norm_w, res, h, workspace, "w8a8_norm_quantize_act")
+    with _on(x, norm_w, res, h, workspace):
+        st = lib().w8a8_norm_quantize_act(_ptr(x), _ptr(res), _ptr(norm_w), _ptr(h), M, K, eps, _ptr(workspace),
+                                          workspace.numel(), _stream())
+    _check(st, "w8a8_norm_quantize_act")
+    return workspace, x if res is None else h
+
+
+def w8a8_norm_linear_fwd(x, norm_w, wq, N, res=None, eps=1e-6, bias=None, workspace=None, h=None, out=None):
+    """(y, h): y bf16 [M, N] = W8A8-linear of the root-mean-square norm of h = x + res, with the weight object `wq` of an
+    [N, K] weight."""
+    M, K, h, workspace = _w8a8_norm_args(x, norm_w, res, h, workspace, "w8a8_norm_linear_fwd")
+    _vector(bias, "bias", N)
+    if wq.dtype != torch.uint8 or not wq.is_contiguous() or wq.numel() < w8a8_weight_bytes(N, K):
+        raise ValueError("wq: expected the weight object of an [%d, %d] weight" % (N, K))
+    out = torch.empty((M, N), dtype=torch.bfloat16, device=x.device) if out is None else out
+    _rows_of(out, "out", (M, N))
+    with _on(x, norm_w, res, h, wq, bias, out, workspace):
+        st = lib().w8a8_norm_linear_fwd(_ptr(x), _ptr(res), _ptr(norm_w), _ptr(h), _ptr(wq), _ptr(bias), _ptr(out), M, N, K, eps,
+                                        _ptr(workspace), workspace.numel(), _stream())
+    _check(st, "w8a8_norm_linear_fwd")
+    return out, x if res is None else h

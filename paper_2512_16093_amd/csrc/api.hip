@@ -8,6 +8,7 @@
 #include <math.h>
 
 #include "common.h"
+#include "host.h"
 
 #include <mutex>
 
@@ -86,26 +87,6 @@ int make_problem(int B, int H, int N, int d, int block_q, int block_k, double rc
   p->lq = p->lk = p->lv = p->lo = p->ld = p->ldq = p->ldk = p->ldv = contiguous_layout(H, N);
   return SLA_OK;
 }
-
-// A caller-given layout: rows of d contiguous channels, 16-byte aligned, at non-negative strides.
-int make_layout(const void* base, const sla_strides* st, int H, int N, Layout* L) {
-  if (!st) {
-    *L = contiguous_layout(H, N);
-    return SLA_OK;
-  }
-  if (st->batch < 0 || st->head < 0 || st->token < D) return SLA_ERR_LAYOUT;
-  if ((st->batch | st->head | st->token) & 7) return SLA_ERR_LAYOUT;
-  if ((uintptr_t)base & 15) return SLA_ERR_LAYOUT;
-  L->sb = st->batch; L->sh = st->head; L->sn = st->token;
-  return SLA_OK;
-}
-
-int check_ws(const void* ws, size_t bytes, size_t need) {
-  if (!ws || ((uintptr_t)ws & 255) || bytes < need) return SLA_ERR_WORKSPACE;
-  return SLA_OK;
-}
-
-int launch_status() { return hipGetLastError() == hipSuccess ? SLA_OK : SLA_ERR_HIP; }
 
 // Optional stage timing of sla_attention_fwd: SLA_N_STAGES + 1 events per recorded call,
 // created by sla_profile_enable and recorded on the call's stream between the stages.
@@ -295,6 +276,7 @@ const char* sla_status_string(int status) {
     case SLA_ERR_HIP: return "a kernel launch failed";
     case SLA_ERR_STATIC_LIMIT: return "problem needs more scratch than the built-in SLA_STATIC_SCRATCH_BYTES";
     case SLA_ERR_LAYOUT: return "unsupported strides (non-negative multiples of 8 elements, token stride >= d, 16-byte aligned base)";
+    case SLA_ERR_VALUE: return "a scalar argument out of range (eps, theta, scale)";
     default: return "unknown status";
   }
 }

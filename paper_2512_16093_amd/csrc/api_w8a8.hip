@@ -5,10 +5,14 @@
 #pragma GCC visibility pop
 
 #include "common.h"
+#include "host.h"
+#include "rows.h"
 
 namespace sla {
 void launch_w8a8_quantize(const void* a, int R, int K, int RP, bool negate_odd, int8_t* codes, float* scales,
                           hipStream_t stream);
+void launch_w8a8_quantize_normed(const void* a, const float* r, const void* w, int R, int K, int RP, int8_t* codes, float* scales,
+                                 hipStream_t stream);
 void launch_w8a8_unpack(const int8_t* frag, const float* s, int R, int K, int RP, bool negate_odd, int8_t* codes,
                         float* scales, hipStream_t stream);
 void launch_w8a8_gemm(const int8_t* x8, const float* sx, int MP, const int8_t* w8, const float* sw,
@@ -26,11 +30,12 @@ bool dims_ok(int R, int K, bool weight) {
 }
 // activations are padded to whole 256-token tiles of the product, weights need no padding
 int padded_rows(int R, bool weight) { return weight ? R : (R + 255) / 256 * 256; }
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // a quantised matrix: codes in operand order, then the block scales
 size_t codes_bytes(int RP, int K) { return align256((size_t)RP * K); }
 size_t object_bytes(int RP, int K) { return codes_bytes(RP, K) + align256((size_t)(RP / 128) * (K / 128) * 4); }
-int launch_status() { return hipGetLastError() == hipSuccess ? SLA_OK : SLA_ERR_HIP; }
+// the norm's factors of the rows lie behind the quantised activations
+bool norm_dims_ok(int M, int K) { return dims_ok(M, K, false) && K <= 16384; }
+size_t norm_bytes(int M, int K) { return object_bytes(padded_rows(M, false), K) + align256((size_t)M * 4); }
 
 }  // namespace
 
@@ -78,6 +83,36 @@ int w8a8_linear_fwd(const void* x, const void* wq, const void* bias, void* y, in
   if (!x || !wq || !y) return SLA_ERR_NULL;
   if (!dims_ok(M, K, false) || !dims_ok(N, K, true)) return SLA_ERR_SHAPE;
   int st = w8a8_quantize_act(x, M, K, workspace, workspace_bytes, stream);
+  if (st != SLA_OK) return st;
+  return w8a8_gemm_fwd(workspace, workspace_bytes, wq, bias, y, M, N, K, stream);
+}
+
+size_t w8a8_norm_workspace_bytes(int M, int K) { return norm_dims_ok(M, K) ? norm_bytes(M, K) : 0; }
+
+int w8a8_norm_quantize_act(const void* x, const void* res, const void* norm_w, void* h, int M, int K, double eps,
+                           void* workspace, size_t workspace_bytes, sla_stream_t stream) {
+  if (!x || !res != !h) return SLA_ERR_NULL;
+  if (!norm_dims_ok(M, K)) return SLA_ERR_SHAPE;
+  if (!eps_ok(eps)) return SLA_ERR_VALUE;
+  if (int st = check_ws(workspace, workspace_bytes, norm_bytes(M, K))) return st;
+  if (!aligned16(x) || !aligned16(res) || !aligned16(norm_w) || !aligned16(h)) return SLA_ERR_LAYOUT;
+  const int MP = padded_rows(M, false);
+  int8_t* codes = (int8_t*)workspace;
+  float* scales = (float*)((unsigned char*)workspace + codes_bytes(MP, K));
+  float* r = (float*)((unsigned char*)workspace + object_bytes(MP, K));
+  launch_norm_stats(x, res, h, r, M, K, (float)eps, (hipStream_t)stream);
+  launch_w8a8_quantize_normed(res ? h : x, r, norm_w, M, K, MP, codes, scales, (hipStream_t)stream);
+  return launch_status();
+}
+
+int w8a8_norm_linear_fwd(const void* x, const void* res, const void* norm_w, void* h, const void* wq, const void* bias,
+                         void* y, int M, int N, int K, double eps, void* workspace, size_t workspace_bytes,
+                         sla_stream_t stream) {
+  if (!x || !res != !h || !wq || !y) return SLA_ERR_NULL;
+  if (!norm_dims_ok(M, K) || !dims_ok(N, K, true)) return SLA_ERR_SHAPE;
+  if ((uintptr_t)wq & 255) return SLA_ERR_WORKSPACE;
+  if (!aligned16(y) || (bias && ((uintptr_t)bias & 7))) return SLA_ERR_LAYOUT;
+  int st = w8a8_norm_quantize_act(x, res, norm_w, h, M, K, eps, workspace, workspace_bytes, stream);
   if (st != SLA_OK) return st;
   return w8a8_gemm_fwd(workspace, workspace_bytes, wq, bias, y, M, N, K, stream);
 }

@@ -51,10 +51,13 @@ __host__ __device__ inline size_t w8_chunk(int kb, int RT, int rt, int ks) {
 // negate_odd (weights): the codes of odd feature blocks are stored negated (see W8_BIAS_I).
 // STREAM: the input is read past the caches (it exceeds what the memory-side cache keeps beside the codes, which the
 // product reads next).
-template <bool STREAM>
+// NORM: what is quantised is x r w, r one factor per row, w (or nothing) one per column: the root-mean-square norm in
+// front of the layer.  It stays in fp32 until its codes, and is never written anywhere.
+template <bool STREAM, bool NORM>
 __global__ void __launch_bounds__(256) w8a8_quantize_kernel(const bf16_t* __restrict__ a, int R, int K, int RP,
                                                             int negate_odd, int8_t* __restrict__ codes,
-                                                            float* __restrict__ scales) {
+                                                            float* __restrict__ scales, const float* __restrict__ row_factor,
+                                                            const bf16_t* __restrict__ col_factor) {
   __shared__ uint4 blk[QB * QB / 16];
   __shared__ float wave_amax[4];
   const int KB = K / QB, RB = RP / QB, RT = RP / 32;
@@ -62,6 +65,23 @@ __global__ void __launch_bounds__(256) w8a8_quantize_kernel(const bf16_t* __rest
   const int t = threadIdx.x, cg = t & 15, r0 = t >> 4, lane = t & 63, w = t >> 6;
   uint4 x[8];
   float amax = 0.f;
+  float rf[8], cf[8];
+  if constexpr (NORM) {
+    if (col_factor) {
+      unpack8(*(const uint4*)(col_factor + kb * QB + cg * 8), cf);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) cf[e] = 1.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rf[i] = rb * QB + r0 + 16 * i < R ? row_factor[rb * QB + r0 + 16 * i] : 0.f;
+  }
+  // column e of this thread's share of row i, given that share's words
+  auto value = [&](int i, const uint32_t (&wd)[4], int e) __attribute__((always_inline)) {
+    const float v = (e & 1) ? bf16_hi(wd[e >> 1]) : bf16_lo(wd[e >> 1]);
+    if constexpr (NORM) return v * rf[i] * cf[e];
+    else return v;
+  };
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int row = rb * QB + r0 + 16 * i;
@@ -72,7 +92,7 @@ __global__ void __launch_bounds__(256) w8a8_quantize_kernel(const bf16_t* __rest
     }
     const uint32_t wd[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(wd[e])), fabsf(bf16_hi(wd[e]))));
+    for (int e = 0; e < 4; ++e) amax = fmaxf(amax, fmaxf(fabsf(value(i, wd, 2 * e)), fabsf(value(i, wd, 2 * e + 1))));
   }
   for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
   if (lane == 0) wave_amax[w] = amax;
@@ -92,8 +112,8 @@ __global__ void __launch_bounds__(256) w8a8_quantize_kernel(const bf16_t* __rest
     uint32_t b[8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      b[2 * e] = int8_code_word_exact(sgn * bf16_lo(wd[e]), cs);
-      b[2 * e + 1] = int8_code_word_exact(sgn * bf16_hi(wd[e]), cs);
+      b[2 * e] = int8_code_word_exact(sgn * value(i, wd, 2 * e), cs);
+      b[2 * e + 1] = int8_code_word_exact(sgn * value(i, wd, 2 * e + 1), cs);
     }
     const uint32_t lo = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u),
                                               __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
@@ -657,9 +677,16 @@ void launch_w8a8_quantize(const void* a, int R, int K, int RP, bool negate_odd, 
   // Above 128 MiB of input the layer gains 1 to 2 % by reading past the caches (75600 x 5120 2.177 -> 2.147 ms,
   // 32760 x 8960 608 -> 591 us); below it loses as much (4096 x 5120 145.6 -> 148.3 us).
   const bool stream_in = (size_t)R * K * 2 > ((size_t)128 << 20);
-#define SLA_QUANTIZE(STREAM) w8a8_quantize_kernel<STREAM><<<grid, 256, 0, stream>>>((const bf16_t*)a, R, K, RP, negate_odd ? 1 : 0, codes, scales)
+#define SLA_QUANTIZE(STREAM) w8a8_quantize_kernel<STREAM, false><<<grid, 256, 0, stream>>>((const bf16_t*)a, R, K, RP, negate_odd ? 1 : 0, codes, scales, nullptr, nullptr)
   if (stream_in) SLA_QUANTIZE(true); else SLA_QUANTIZE(false);
 #undef SLA_QUANTIZE
+}
+
+// The same of x r w (r fp32 [R], w bf16 [K] or nullptr).
+void launch_w8a8_quantize_normed(const void* a, const float* r, const void* w, int R, int K, int RP, int8_t* codes, float* scales,
+                                 hipStream_t stream) {
+  w8a8_quantize_kernel<false, true><<<(unsigned)((RP / QB) * (K / QB)), 256, 0, stream>>>((const bf16_t*)a, R, K, RP, 0, codes, scales,
+                                                                                        r, (const bf16_t*)w);
 }
 
 void launch_w8a8_unpack(const int8_t* frag, const float* s, int R, int K, int RP, bool negate_odd, int8_t* codes,
