@@ -35,6 +35,7 @@ W8A8_EXPORTS = ("w8a8_weight_bytes", "w8a8_quantize_weight", "w8a8_workspace_byt
                 "w8a8_quantize_act", "w8a8_gemm_fwd", "w8a8_debug_unpack", "w8a8_norm_workspace_bytes",
                 "w8a8_norm_quantize_act", "w8a8_norm_linear_fwd")
 ROPE_EXPORTS = ("rope_make_plan", "rope_qk_fwd", "rope_bwd_workspace_bytes", "rope_qk_bwd")
+XATTN_EXPORTS = ("xattn_workspace_bytes", "xattn_fwd", "xattn_bwd_workspace_bytes", "xattn_bwd")
 NORM_EXPORTS = ("norm_rms_fwd", "norm_bwd_workspace_bytes", "norm_rms_bwd")
 BWD_EXPORTS = ("sla_bwd_workspace_bytes", "sla_attention_bwd", "sla_saved_bytes", "sla_attention_fwd_train",
                "sla_attention_bwd_saved", "sla_attention_fwd_train_strided", "sla_attention_bwd_strided")
@@ -63,6 +64,11 @@ class RopePlan(ctypes.Structure):
 class RopeBwdStrides(ctypes.Structure):
     """rope_bwd_strides of include/rope.h."""
     _fields_ = [(n, ctypes.POINTER(Strides)) for n in ("dq_out", "dk_out", "q", "k", "dq", "dk")]
+
+
+class XattnBwdStrides(ctypes.Structure):
+    """xattn_bwd_strides of include/xattn.h."""
+    _fields_ = [(n, ctypes.POINTER(Strides)) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
 
 
 class SLAError(RuntimeError):
@@ -180,6 +186,14 @@ def lib():
         L.norm_bwd_workspace_bytes.argtypes = [c_int] * 2
         L.norm_rms_bwd.restype = c_int
         L.norm_rms_bwd.argtypes = [c_vp] * 6 + [c_int] * 2 + [c_dbl, c_vp, c_sz, c_vp]
+        # include/xattn.h
+        for f in (L.xattn_workspace_bytes, L.xattn_bwd_workspace_bytes):
+            f.restype = c_sz
+            f.argtypes = [c_int] * 6
+        L.xattn_fwd.restype = c_int
+        L.xattn_fwd.argtypes = [c_vp] * 5 + [sp] * 4 + [c_vp] + [c_int] * 6 + [c_dbl, c_vp, c_sz, c_vp]
+        L.xattn_bwd.restype = c_int
+        L.xattn_bwd.argtypes = ([c_vp] * 9 + [ctypes.POINTER(XattnBwdStrides), c_vp] + [c_int] * 6 + [c_dbl, c_vp, c_sz, c_vp])
         _lib = L
     return _lib
 
@@ -819,3 +833,55 @@ def w8a8_norm_linear_fwd(x, norm_w, wq, N, res=None, eps=1e-6, bias=None, worksp
                                         _ptr(workspace), workspace.numel(), _stream())
     _check(st, "w8a8_norm_linear_fwd")
     return out, x if res is None else h
+
+
+# ---------------------------------------------------------------------------
+# include/xattn.h
+# ---------------------------------------------------------------------------
+def xattn_workspace_bytes(B, H, Hkv, Nq, Nk, d):
+    return lib().xattn_workspace_bytes(B, H, Hkv, Nq, Nk, d)
+
+
+def xattn_bwd_workspace_bytes(B, H, Hkv, Nq, Nk, d):
+    return lib().xattn_bwd_workspace_bytes(B, H, Hkv, Nq, Nk, d)
+
+
+def _xattn_args(q, k, v, k_lens, scale):
+    """(B, H, Hkv, Nq, Nk, d), scale as the library takes it (0: 1 / sqrt(d))"""
+    B, H, Nq, d = q.shape
+    if k.dim() != 4 or k.shape[0] != B or k.shape[3] != d or v.shape != k.shape:
+        raise ValueError("q [B,H,Nq,d], k and v [B,Hkv,Nk,d] with the same B and d")
+    _vector(k_lens, "k_lens", B, torch.int32)
+    if scale is not None and not scale > 0:
+        raise ValueError("scale: expected a number above 0, or None for 1 / sqrt(d)")
+    return (B, H, k.shape[1], Nq, k.shape[2], d), 0.0 if scale is None else scale
+
+
+def xattn_fwd(q, k, v, k_lens=None, scale=None, out=None, want_lse=False, workspace=None):
+    """(out, lse fp32 [B,H,Nq] or None): attention of q [B,H,Nq,d] to k, v [B,Hkv,Nk,d] (any memory order with contiguous
+    channels; H a multiple of Hkv), of each sample's first k_lens (int32 [B]; None: all) keys."""
+    dims, scale = _xattn_args(q, k, v, k_lens, scale)
+    out = _heads_like(q) if out is None else out
+    lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
+    s = [_strides_or_none(t, n, like) for t, n, like in ((q, "q", q), (k, "k", k), (v, "v", k), (out, "out", q))]
+    workspace = _scratch(workspace, lib().xattn_workspace_bytes(*dims), q.device, "xattn_fwd")
+    with _on(q, k, v, out, k_lens, workspace):
+        st = lib().xattn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), *s, _ptr(k_lens), *dims, scale, _ptr(workspace),
+                             workspace.numel(), _stream())
+    _check(st, "xattn_fwd")
+    return out, lse
+
+
+def xattn_bwd(q, k, v, out, dout, lse, k_lens=None, scale=None, grads=None, workspace=None):
+    """(dq, dk, dv) bf16 of xattn_fwd, whose out and lse these are; `grads` may hand in the three tensors."""
+    dims, scale = _xattn_args(q, k, v, k_lens, scale)
+    _vector(lse, "lse", dims[0] * dims[1] * dims[3], torch.float32)
+    dq, dk, dv = (_heads_like(t) for t in (q, k, k)) if grads is None else grads
+    named = ((q, "q", q), (k, "k", k), (v, "v", k), (out, "out", q), (dout, "dout", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k))
+    s = XattnBwdStrides(*[_strides_or_none(*x) for x in named])
+    workspace = _scratch(workspace, lib().xattn_bwd_workspace_bytes(*dims), q.device, "xattn_bwd")
+    with _on(q, k, v, out, dout, lse, dq, dk, dv, k_lens, workspace):
+        st = lib().xattn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(dout), _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv),
+                             ctypes.byref(s), _ptr(k_lens), *dims, scale, _ptr(workspace), workspace.numel(), _stream())
+    _check(st, "xattn_bwd")
+    return dq, dk, dv

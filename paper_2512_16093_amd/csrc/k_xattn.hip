@@ -1,0 +1,577 @@
+// Attention to a sequence of another length (include/xattn.h), forward and backward.
+//
+//   xattn_fwd_kernel     per 32 to 128 query rows, over the keys: one pass with a running maximum and sum.
+//   xattn_join_kernel    joins the pieces of a walk that was split: weights 2^(m - max m), one division.
+//   xattn_delta_kernel   delta = dout . out and the base-2 log-sum-exp, padded to whole steps of the dk, dv walk.
+//   xattn_dq_kernel      per 32 to 128 query rows, over the keys: dQ += dS K.
+//   xattn_dkv_kernel     per 32 to 128 keys, over the query rows of every head that shares them: dV += P^T dO, dK += dS^T Q.
+//   xattn_sum_kernel     adds up the pieces of split walks of the two.
+//
+// All products are formed transposed where that saves a shuffle: a wavefront owns 32 rows, one per lane pair, so a row's
+// statistics stay inside the pair, and an accumulator tile converted to bf16 is the B operand of the next product (its
+// contraction index = the accumulator's rows).  Tiles of 32 rows are copied to LDS one step ahead (tiles.h).
+//
+// A key head's query rows are those of all heads that share it, head after head, so that its keys are read once for all of
+// them.  Where the rows do not fill the chip (few tokens against a long memory) the walk is split and joined through the
+// workspace.
+#include <algorithm>
+#include <cfloat>
+
+#include "tiles.h"
+#include "xattn.h"
+
+namespace sla {
+
+// Consecutive workgroups go to the eight XCDs in turn: each XCD gets a contiguous eighth of the units, so that the
+// workgroups on it at a time work on neighbouring ones (the same slice's keys).  False: no unit.
+__device__ __forceinline__ bool xattn_unit(long long units, long long& unit) {
+  const long long per = (units + 7) >> 3, slot = blockIdx.x >> 3;
+  unit = (blockIdx.x & 7) * per + slot;
+  return slot < per && unit < units;
+}
+static unsigned xattn_grid(long long units) { return (unsigned)(8 * ((units + 7) / 8)); }
+
+__device__ __forceinline__ int xattn_len(const XattnArgs& a, int b) {
+  return a.lens ? min(max(__builtin_amdgcn_readfirstlane(a.lens[b]), 0), a.Nk) : a.Nk;
+}
+
+// Query row r of a key head (head after head): its place in a tensor laid out by L.
+struct QueryRows {
+  long long base, sh, sn;
+  int Nq;
+  __device__ __forceinline__ QueryRows(const XattnArgs& a, const Layout& L, int b, int g)
+      : base(b * L.sb + (long long)g * a.group * L.sh), sh(L.sh), sn(L.sn), Nq(a.Nq) {}
+  __device__ __forceinline__ long long at(int r) const {
+    const int head = (unsigned)r / (unsigned)Nq;
+    return base + head * sh + (long long)(r - head * Nq) * sn;
+  }
+};
+// The 32 rows of a wavefront as operands; rows that do not exist are zeros.
+__device__ __forceinline__ void query_operands(const bf16_t* x, const QueryRows& at, int r, int rows, int hf, uint4 (&f)[8]) {
+  const bf16_t* p = x + at.at(min(r, rows - 1));
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) f[ks] = r < rows ? *(const uint4*)(p + 16 * ks + 8 * hf) : uint4{0u, 0u, 0u, 0u};
+}
+// A wavefront's 32 rows x 128 channels (lane = row, registers = channels) out: in whole rows where they lie in one head, as
+// store_rows; else row by row.
+__device__ __forceinline__ void store_query_rows(unsigned char* lds, const v16f (&x)[4], int lane, bf16_t* to, const QueryRows& at, int r0, int rows) {
+  if (r0 >= rows) return;
+  const int last = min(r0 + 31, rows - 1);
+  if ((unsigned)r0 / (unsigned)at.Nq == (unsigned)last / (unsigned)at.Nq) {
+    store_rows(lds, x, lane, to + at.at(r0), at.sn, last - r0 + 1);
+    return;
+  }
+  const int r = r0 + (lane & 31), hf = lane >> 5;
+  if (r < rows) {
+    bf16_t* p = to + at.at(r) + 4 * hf;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(uint2*)(p + 32 * ct + 8 * g) = uint2{pack_bf16x2(x[ct][4 * g], x[ct][4 * g + 1]), pack_bf16x2(x[ct][4 * g + 2], x[ct][4 * g + 3])};
+  }
+}
+// The same as fp32 rows of a partial result.
+__device__ __forceinline__ void store_partial(float* row, const v16f (&x)[4], int hf) {
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *(float4*)(row + 32 * ct + 8 * g + 4 * hf) = float4{x[ct][4 * g], x[ct][4 * g + 1], x[ct][4 * g + 2], x[ct][4 * g + 3]};
+}
+
+// LSE: the log-sum-exp is wanted too (of the unrounded weights: its own sum).  SPLIT: a piece of the walk, to the workspace.
+template <int NW, bool LSE, bool SPLIT>
+__global__ void __launch_bounds__(NW * 64, 2) xattn_fwd_kernel(XattnArgs a) {
+  constexpr int KT = NW == 4 ? 2 : 1, STEP_B = 2 * KT * SWZ_TILE_B, STEP = 32 * KT;
+  __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];   // two steps' tiles: KT of K, then KT of V
+  long long unit;
+  if (!xattn_unit((long long)a.B * a.G * a.fwd.splits * a.fwd.tiles, unit)) return;
+  const int tile = (int)(unit % a.fwd.tiles), rest = (int)(unit / a.fwd.tiles);
+  const int split = SPLIT ? rest % a.fwd.splits : 0, bg = SPLIT ? rest / a.fwd.splits : rest;
+  const int b = bg / a.G, g = bg - b * a.G;
+  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
+  const int len = xattn_len(a, b), k0 = SPLIT ? split * a.fwd.chunk : 0, k1 = SPLIT ? min(len, k0 + a.fwd.chunk) : len;
+  const int r0 = (tile * NW + w) * 32, row = r0 + l32;
+  uint4 qf[8];
+  query_operands(a.q, QueryRows(a, a.lq, b, g), row, a.rows, hf, qf);
+  v16f o[4];
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct) o[ct] = v16f{};
+  float m = -FLT_MAX, lx = 0.f;
+  v16f lacc = v16f{};    // register 0: the running sum of the rounded weights
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
+  if (k0 < k1) {
+    TileCopy<NW> ck, cv;
+    ck.init(a.k + b * a.lk.sb + g * a.lk.sh, a.lk.sn, w, lane);
+    cv.init(a.v + b * a.lv.sb + g * a.lv.sh, a.lv.sn, w, lane);
+    const int n_off = swz_lane_offset(l32, hf), t_off = swz_tr_lane_offset(lane);
+    auto request = [&](int key0, int half) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        ck.tile(key0 + 32 * kt, len, lds0 + half * STEP_B + kt * SWZ_TILE_B);
+        cv.template tile<true>(key0 + 32 * kt, len, lds0 + half * STEP_B + (KT + kt) * SWZ_TILE_B);   // (zero times what lies there need not be zero)
+      }
+    };
+    request(k0, 0);
+    int half = 0;
+    for (int key0 = k0; key0 < k1; key0 += STEP, half ^= 1) {
+      copies_barrier<0>();                     // this step's tiles have landed; those of the step before are consumed
+      if (key0 + STEP < k1) request(key0 + STEP, half ^ 1);
+      int no = n_off + half * STEP_B, to = t_off + half * STEP_B;
+      asm volatile("" : "+v"(no), "+v"(to));
+      v16f s[KT];
+      float mx = -INFINITY;
+      uint4 ak[8], tv[2][4];
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) ak[ks] = n_op_swz(ring, no, ks);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        s[kt] = v16f{};
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {       // behind a product: the read of the next tile's operand, at the end V's first ones
+          s[kt] = mfma_bf16(ak[ks], qf[ks], s[kt]);
+          if (kt + 1 < KT) ak[ks] = n_op_swz(ring + (kt + 1) * SWZ_TILE_B, no, ks);
+          else if (ks >= 4) tv[0][ks - 4] = t_op_swz(ring + KT * SWZ_TILE_B, to, ks - 4, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        if (key0 + 32 * kt + 32 > k1) {        // (uniform) the last tile can hold keys that do not exist
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (key0 + 32 * kt + 8 * (r >> 2) + 4 * hf + (r & 3) >= k1) s[kt][r] = -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kt][r]);
+      }
+      // The reference m moves only when the tiles' maximum exceeds it by more than 2^8: the weights then stay below 2^8
+      // (harmless in bf16 and fp32) and the accumulators are rescaled a few times per row instead of every step.
+      if (__any(mx * a.c2 > m + 8.0f)) {
+        mx = fmaxf(mx, partner_f32(mx)) * a.c2;
+        const float m_new = mx > m + 8.0f ? mx : m;
+        const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        lacc[0] *= alpha;
+        if constexpr (LSE) lx *= alpha;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
+      }
+      auto weight = [&](int e) __attribute__((always_inline)) {   // of element e % 16 of tile e / 16
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], a.c2, -m));
+        s[e >> 4][e & 15] = p;
+        if constexpr (LSE) lx += p;
+      };
+      const uint4 ones = uint4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};  // bf16 1.0: sums the weights over the keys
+#pragma unroll
+      for (int e = 0; e < 8; ++e) weight(e);
+#pragma unroll
+      for (int u = 0; u < 2 * KT; ++u) {       // 16 keys; behind their products the next ones' exponentials and operand reads
+        const uint4 pb = acc_operand(s[u >> 1], u & 1);
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) {
+          o[ct] = mfma_bf16(tv[u & 1][ct], pb, o[ct]);
+          if (u + 1 < 2 * KT) {
+            tv[(u + 1) & 1][ct] = t_op_swz(ring + (KT + ((u + 1) >> 1)) * SWZ_TILE_B, to, ct, (u + 1) & 1);
+            weight(8 * u + 8 + 2 * ct);
+            weight(8 * u + 9 + 2 * ct);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        lacc = mfma_bf16(ones, pb, lacc);
+      }
+    }
+  }
+  const float l = lacc[0];                     // (0: no key)
+  if constexpr (LSE) lx += partner_f32(lx);
+  const long long first = ((long long)b * a.H + g * a.group) * a.Nq;   // of this key head's query rows among all
+  if constexpr (SPLIT) {
+    if (row < a.rows) {
+      const long long at = (long long)split * a.B * a.H * a.Nq + first + row;
+      if (hf == 0) *(float4*)(a.part_ml + 4 * at) = float4{m, l, LSE ? lx : l, 0.f};
+      store_partial(a.part_o + at * D, o, hf);
+    }
+  } else {
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[ct][r] *= inv;
+    if constexpr (LSE) {
+      if (hf == 0 && row < a.rows) a.lse[first + row] = l > 0.f ? (m + __builtin_amdgcn_logf(lx)) * LN2 : -INFINITY;
+    }
+    copies_barrier<0>();                       // nobody reads the last step's tiles any more
+    store_query_rows(ring + w * 8192, o, lane, a.out, QueryRows(a, a.lo, b, g), r0, a.rows);
+  }
+}
+
+// Eight rows per workgroup, half a wavefront each; or (WIDE) one row, its pieces dealt to the eight halves.
+template <bool WIDE>
+__global__ void __launch_bounds__(256) xattn_join_kernel(XattnArgs a) {
+  __shared__ float4 red_o[8][32];
+  __shared__ float2 red_l[8];
+  const int t = threadIdx.x, half = t >> 5, c = t & 31;
+  const long long all = (long long)a.B * a.H * a.Nq, row = WIDE ? blockIdx.x : 8ll * blockIdx.x + half;
+  if (row >= all) return;                      // (WIDE: of the whole workgroup)
+  const int S = a.fwd.splits;
+  float M = -FLT_MAX;
+  for (int s = 0; s < S; ++s) {
+    const float4 ml = *(const float4*)(a.part_ml + 4 * (s * all + row));
+    if (ml.y > 0.f) M = fmaxf(M, ml.x);
+  }
+  float4 o{0.f, 0.f, 0.f, 0.f};
+  float2 l{0.f, 0.f};
+#pragma unroll 4
+  for (int s = WIDE ? half : 0; s < S; s += WIDE ? 8 : 1) {
+    const float4 ml = *(const float4*)(a.part_ml + 4 * (s * all + row));
+    const float w = ml.y > 0.f ? __builtin_amdgcn_exp2f(ml.x - M) : 0.f;
+    const float4 p = *(const float4*)(a.part_o + (s * all + row) * D + 4 * c);
+    o.x = __builtin_fmaf(w, p.x, o.x); o.y = __builtin_fmaf(w, p.y, o.y);
+    o.z = __builtin_fmaf(w, p.z, o.z); o.w = __builtin_fmaf(w, p.w, o.w);
+    l.x = __builtin_fmaf(w, ml.y, l.x);
+    l.y = __builtin_fmaf(w, ml.z, l.y);
+  }
+  if constexpr (WIDE) {
+    red_o[half][c] = o;
+    if (c == 0) red_l[half] = l;
+    __syncthreads();
+    if (half != 0) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+      const float4 p = red_o[i][c];
+      o.x += p.x; o.y += p.y; o.z += p.z; o.w += p.w;
+      l.x += red_l[i].x;
+      l.y += red_l[i].y;
+    }
+  }
+  const float inv = l.x > 0.f ? 1.0f / l.x : 0.f;
+  const long long bh = row / a.Nq;
+  const int n = (int)(row - bh * a.Nq), b = (int)(bh / a.H), h = (int)(bh - (long long)b * a.H);
+  *(uint2*)(a.out + b * a.lo.sb + h * a.lo.sh + n * a.lo.sn + 4 * c) = uint2{pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv)};
+  if (a.lse && c == 0) a.lse[row] = l.x > 0.f ? (M + __builtin_amdgcn_logf(l.y)) * LN2 : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------
+// Sixteen rows per workgroup, sixteen lanes each.  Rows that pad a head to whole steps, and rows without keys: lse = +infinity, so
+// that their weights are exactly zero.
+__global__ void __launch_bounds__(256) xattn_delta_kernel(XattnArgs a) {
+  const int padded = xattn_padded_rows(a.Nq), part = threadIdx.x & 15;
+  const long long i = 16ll * blockIdx.x + (threadIdx.x >> 4);
+  const long long bh = i / padded;
+  const int n = (int)(i - bh * padded), b = (int)(bh / a.H), h = (int)(bh - (long long)b * a.H);
+  float dot = 0.f, lse2 = INFINITY;
+  if (n < a.Nq) {
+    float x[8], y[8];
+    unpack8(*(const uint4*)(a.o + b * a.lo.sb + h * a.lo.sh + n * a.lo.sn + 8 * part), x);
+    unpack8(*(const uint4*)(a.dout + b * a.ldo.sb + h * a.ldo.sh + n * a.ldo.sn + 8 * part), y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(x[e], y[e], dot);
+    const float l = a.lse_in[bh * a.Nq + n];
+    if (l > -INFINITY) lse2 = l * LOG2E;
+  }
+  dot = row_sum(dot);
+  if (part == 0) {
+    a.delta[i] = dot;
+    a.lse2[i] = lse2;
+  }
+}
+
+template <int NW, bool SPLIT>
+__global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
+  constexpr int KT = NW == 4 ? 2 : 1, STEP_B = 2 * KT * SWZ_TILE_B, STEP = 32 * KT;
+  __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];
+  long long unit;
+  if (!xattn_unit((long long)a.B * a.G * a.dqd.splits * a.dqd.tiles, unit)) return;
+  const int tile = (int)(unit % a.dqd.tiles), rest = (int)(unit / a.dqd.tiles);
+  const int split = SPLIT ? rest % a.dqd.splits : 0, bg = SPLIT ? rest / a.dqd.splits : rest;
+  const int b = bg / a.G, g = bg - b * a.G;
+  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
+  const int len = xattn_len(a, b), k0 = SPLIT ? split * a.dqd.chunk : 0, k1 = SPLIT ? min(len, k0 + a.dqd.chunk) : len;
+  const int r0 = (tile * NW + w) * 32, row = r0 + l32;
+  v16f dq[4];
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct) dq[ct] = v16f{};
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
+  if (k0 < k1) {
+    uint4 qf[8], df[8];
+    query_operands(a.q, QueryRows(a, a.lq, b, g), row, a.rows, hf, qf);
+    query_operands(a.dout, QueryRows(a, a.ldo, b, g), row, a.rows, hf, df);
+    float lse2 = INFINITY, delta = 0.f;
+    if (row < a.rows) {
+      const int head = (unsigned)row / (unsigned)a.Nq;
+      const long long at = ((long long)b * a.H + g * a.group + head) * xattn_padded_rows(a.Nq) + (row - head * a.Nq);
+      lse2 = a.lse2[at];
+      delta = a.delta[at];
+    }
+    TileCopy<NW> ck, cv;
+    ck.init(a.k + b * a.lk.sb + g * a.lk.sh, a.lk.sn, w, lane);
+    cv.init(a.v + b * a.lv.sb + g * a.lv.sh, a.lv.sn, w, lane);
+    const int n_off = swz_lane_offset(l32, hf), t_off = swz_tr_lane_offset(lane);
+    // (keys behind the last come as the last one: their weights are zero)
+    auto request = [&](int key0, int half) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        ck.tile(key0 + 32 * kt, len, lds0 + half * STEP_B + kt * SWZ_TILE_B);
+        cv.tile(key0 + 32 * kt, len, lds0 + half * STEP_B + (KT + kt) * SWZ_TILE_B);
+      }
+    };
+    request(k0, 0);
+    int half = 0;
+    for (int key0 = k0; key0 < k1; key0 += STEP, half ^= 1) {
+      copies_barrier<0>();
+      if (key0 + STEP < k1) request(key0 + STEP, half ^ 1);
+      int no = n_off + half * STEP_B, to = t_off + half * STEP_B;
+      asm volatile("" : "+v"(no), "+v"(to));
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        const unsigned char *tk = ring + kt * SWZ_TILE_B, *tv = ring + (KT + kt) * SWZ_TILE_B;
+        v16f s = v16f{}, dp;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] = -delta;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          s = mfma_bf16(n_op_swz(tk, no, ks), qf[ks], s);
+          dp = mfma_bf16(n_op_swz(tv, no, ks), df[ks], dp);
+        }
+        if (key0 + 32 * kt + 32 > k1) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (key0 + 32 * kt + 8 * (r >> 2) + 4 * hf + (r & 3) >= k1) s[r] = -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c2, -lse2)) * dp[r];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint4 ds = acc_operand(s, u);
+#pragma unroll
+          for (int ct = 0; ct < 4; ++ct) dq[ct] = mfma_bf16(t_op_swz(tk, to, ct, u), ds, dq[ct]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dq[ct][r] *= a.scale;
+  if constexpr (SPLIT) {
+    if (row < a.rows)
+      store_partial(a.part_dq + ((long long)split * a.B * a.H * a.Nq + ((long long)b * a.H + g * a.group) * a.Nq + row) * D, dq, hf);
+  } else {
+    copies_barrier<0>();
+    store_query_rows(ring + w * 8192, dq, lane, a.dq, QueryRows(a, a.ldq, b, g), r0, a.rows);
+  }
+}
+
+// A wavefront owns 32 keys and walks over the query rows of every head of its group, 32 QT rows a step.
+template <int NW, bool SPLIT>
+__global__ void __launch_bounds__(NW * 64, 1) xattn_dkv_kernel(XattnArgs a) {
+  constexpr int QT = 2, STEP_B = 2 * QT * SWZ_TILE_B + 512, STEP = 32 * QT;   // Q, dO, then lse2 and delta of the rows
+  __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];
+  long long unit;
+  if (!xattn_unit((long long)a.B * a.G * a.dkv.splits * a.dkv.tiles, unit)) return;
+  const int tile = (int)(unit % a.dkv.tiles), rest = (int)(unit / a.dkv.tiles);
+  const int split = SPLIT ? rest % a.dkv.splits : 0, bg = SPLIT ? rest / a.dkv.splits : rest;
+  const int b = bg / a.G, g = bg - b * a.G;
+  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
+  const int len = xattn_len(a, b), key0 = (tile * NW + w) * 32, key = key0 + l32;
+  const int per_head = (a.Nq + STEP - 1) / STEP, total = a.group * per_head;
+  const int s0 = SPLIT ? split * a.dkv.chunk : 0, s1 = SPLIT ? min(total, s0 + a.dkv.chunk) : total;
+  v16f dk[4], dv[4];
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct) dk[ct] = dv[ct] = v16f{};
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
+  if (tile * NW * 32 < len && s0 < s1) {       // (uniform)
+    uint4 kf[8], vf[8];
+    own_rows(a.k + b * a.lk.sb + g * a.lk.sh, a.lk.sn, key, len, hf, kf);
+    own_rows(a.v + b * a.lv.sb + g * a.lv.sh, a.lv.sn, key, len, hf, vf);
+    TileCopy<NW> cq, cd;
+    const bf16_t *q0 = a.q + b * a.lq.sb + (long long)g * a.group * a.lq.sh, *d0 = a.dout + b * a.ldo.sb + (long long)g * a.group * a.ldo.sh;
+    cq.init(q0, a.lq.sn, w, lane);
+    cd.init(d0, a.ldo.sn, w, lane);
+    const long long stat0 = ((long long)b * a.H + g * a.group) * xattn_padded_rows(a.Nq);
+    const int n_off = swz_lane_offset(l32, hf), t_off = swz_tr_lane_offset(lane);
+    int head = s0 / per_head, in_head = s0 - head * per_head;   // of the step requested next
+    auto request = [&](int half) __attribute__((always_inline)) {
+      cq.slice = (const char*)(q0 + head * a.lq.sh);
+      cd.slice = (const char*)(d0 + head * a.ldo.sh);
+      const int row0 = in_head * STEP;
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {           // (rows behind a head's last come as its last: their weights are zero)
+        cq.tile(row0 + 32 * x, a.Nq, lds0 + half * STEP_B + x * SWZ_TILE_B);
+        cd.tile(row0 + 32 * x, a.Nq, lds0 + half * STEP_B + (QT + x) * SWZ_TILE_B);
+      }
+      if (w == 0) {
+        const long long at = stat0 + (long long)head * xattn_padded_rows(a.Nq) + row0;
+        copy_floats(a.lse2 + at, 4u * lane, lds0 + half * STEP_B + 2 * QT * SWZ_TILE_B);
+        copy_floats(a.delta + at, 4u * lane, lds0 + half * STEP_B + 2 * QT * SWZ_TILE_B + 256);
+      }
+      if (++in_head == per_head) {
+        in_head = 0;
+        ++head;
+      }
+    };
+    request(0);
+    int half = 0;
+    for (int step = s0; step < s1; ++step, half ^= 1) {
+      copies_barrier<0>();
+      if (step + 1 < s1) request(half ^ 1);
+      int no = n_off + half * STEP_B, to = t_off + half * STEP_B;
+      asm volatile("" : "+v"(no), "+v"(to));
+      const unsigned char* stat = ring + half * STEP_B + 2 * QT * SWZ_TILE_B + 16 * hf;
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        const unsigned char *tq = ring + x * SWZ_TILE_B, *td = ring + (QT + x) * SWZ_TILE_B;
+        v16f s = v16f{}, dp;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {          // (rows 8 u + 4 hf + 0..3 of the tile)
+          const float4 d4 = *(const float4*)(stat + 256 + 128 * x + 32 * u);
+          dp[4 * u] = -d4.x; dp[4 * u + 1] = -d4.y; dp[4 * u + 2] = -d4.z; dp[4 * u + 3] = -d4.w;
+        }
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          s = mfma_bf16(n_op_swz(tq, no, ks), kf[ks], s);
+          dp = mfma_bf16(n_op_swz(td, no, ks), vf[ks], dp);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float4 l4 = *(const float4*)(stat + 128 * x + 32 * u);
+          const float lr[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[4 * u + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * u + e], a.c2, -lr[e]));
+            dp[4 * u + e] *= s[4 * u + e];
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint4 pb = acc_operand(s, u), db = acc_operand(dp, u);
+#pragma unroll
+          for (int ct = 0; ct < 4; ++ct) {
+            dv[ct] = mfma_bf16(t_op_swz(td, to, ct, u), pb, dv[ct]);
+            dk[ct] = mfma_bf16(t_op_swz(tq, to, ct, u), db, dk[ct]);
+          }
+        }
+      }
+    }
+  }
+  const float keep = key < len ? a.scale : 0.f;
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      dk[ct][r] = key < len ? dk[ct][r] * keep : 0.f;      // (a key that does not exist took whatever weights zeros give)
+      dv[ct][r] = key < len ? dv[ct][r] : 0.f;
+    }
+  if constexpr (SPLIT) {
+    if (key < a.Nk) {
+      const long long at = (((long long)split * a.B + b) * a.G + g) * a.Nk + key;
+      store_partial(a.part_dk + at * D, dk, hf);
+      store_partial(a.part_dv + at * D, dv, hf);
+    }
+  } else {
+    copies_barrier<0>();
+    if (key0 < a.Nk) {
+      unsigned char* mine = ring + w * 8192;
+      store_rows(mine, dk, lane, a.dk + b * a.ldk.sb + g * a.ldk.sh + key0 * a.ldk.sn, a.ldk.sn, a.Nk - key0);
+      store_rows(mine, dv, lane, a.dv + b * a.ldv.sb + g * a.ldv.sh + key0 * a.ldv.sn, a.ldv.sn, a.Nk - key0);
+    }
+  }
+}
+
+// to[b][h][n] = sum over s of part[s][b][h][n], eight rows per workgroup; blockIdx.y: which of two tensors.
+struct XattnSum {
+  const float* part[2];
+  bf16_t* to[2];
+  Layout L[2];
+  int splits, H, N;
+  long long rows;
+};
+__global__ void __launch_bounds__(256) xattn_sum_kernel(XattnSum x) {
+  const int c = threadIdx.x & 31, y = blockIdx.y;
+  const long long row = 8ll * blockIdx.x + (threadIdx.x >> 5);
+  if (row >= x.rows) return;
+  float4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < x.splits; ++s) {
+    const float4 p = *(const float4*)(x.part[y] + (s * x.rows + row) * D + 4 * c);
+    o.x += p.x; o.y += p.y; o.z += p.z; o.w += p.w;
+  }
+  const long long bh = row / x.N;
+  const int n = (int)(row - bh * x.N), b = (int)(bh / x.H), h = (int)(bh - (long long)b * x.H);
+  *(uint2*)(x.to[y] + b * x.L[y].sb + h * x.L[y].sh + n * x.L[y].sn + 4 * c) = uint2{pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w)};
+}
+
+// ---------------------------------------------------------------------------
+static XattnDeal deal(long long units, int nw, int tiles, int walk, int step, int least, long long places) {
+  // As many pieces as there are places for, none shorter than `least`.
+  const long long most = std::max<long long>(1, walk / least), want = std::max<long long>(1, places / std::max<long long>(1, units));
+  const int pieces = (int)std::min(most, want);
+  int chunk = (walk + pieces - 1) / pieces;
+  chunk = (chunk + step - 1) / step * step;
+  return XattnDeal{nw, tiles, (walk + chunk - 1) / chunk, chunk};
+}
+XattnDeal xattn_deal_rows(int B, int G, int rows, int Nk) {
+  const int nw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4, tiles = (rows + 32 * nw - 1) / (32 * nw);
+  return deal((long long)B * G * tiles, nw, tiles, Nk, nw == 4 ? 64 : 32, 256, (long long)compute_units() * (nw == 4 ? 2 : 4));
+}
+XattnDeal xattn_deal_keys(int B, int G, int group, int Nq, int Nk) {
+  const int nw = Nk <= 32 ? 1 : Nk <= 64 ? 2 : 4, tiles = (Nk + 32 * nw - 1) / (32 * nw);
+  return deal((long long)B * G * tiles, nw, tiles, group * ((Nq + 63) / 64), 1, 4, (long long)compute_units() * (nw == 4 ? 1 : 2));
+}
+
+void launch_xattn_fwd(const XattnArgs& a, hipStream_t stream) {
+  const long long units = (long long)a.B * a.G * a.fwd.splits * a.fwd.tiles;
+#define XATTN_FWD(NW)                                                                                                          \
+  do {                                                                                                                         \
+    if (a.fwd.splits > 1) {                                                                                                    \
+      if (a.lse) xattn_fwd_kernel<NW, true, true><<<xattn_grid(units), NW * 64, 0, stream>>>(a);                               \
+      else xattn_fwd_kernel<NW, false, true><<<xattn_grid(units), NW * 64, 0, stream>>>(a);                                    \
+    } else {                                                                                                                   \
+      if (a.lse) xattn_fwd_kernel<NW, true, false><<<xattn_grid(units), NW * 64, 0, stream>>>(a);                              \
+      else xattn_fwd_kernel<NW, false, false><<<xattn_grid(units), NW * 64, 0, stream>>>(a);                                   \
+    }                                                                                                                          \
+  } while (0)
+  if (a.fwd.nw == 1) XATTN_FWD(1);
+  else if (a.fwd.nw == 2) XATTN_FWD(2);
+  else XATTN_FWD(4);
+#undef XATTN_FWD
+  if (a.fwd.splits > 1) {
+    const long long all = (long long)a.B * a.H * a.Nq;
+    if (a.fwd.splits > 8) xattn_join_kernel<true><<<(unsigned)all, 256, 0, stream>>>(a);
+    else xattn_join_kernel<false><<<(unsigned)((all + 7) / 8), 256, 0, stream>>>(a);
+  }
+}
+
+void launch_xattn_bwd(const XattnArgs& a, hipStream_t stream) {
+  const long long all = (long long)a.B * a.H * a.Nq, padded = (long long)a.B * a.H * xattn_padded_rows(a.Nq);
+  xattn_delta_kernel<<<(unsigned)(padded / 16), 256, 0, stream>>>(a);
+  const unsigned gq = xattn_grid((long long)a.B * a.G * a.dqd.splits * a.dqd.tiles), gk = xattn_grid((long long)a.B * a.G * a.dkv.splits * a.dkv.tiles);
+#define XATTN_BWD(KERNEL, NW, SPLIT, GRID)                                    \
+  do {                                                                        \
+    if (SPLIT) KERNEL<NW, true><<<GRID, NW * 64, 0, stream>>>(a);             \
+    else KERNEL<NW, false><<<GRID, NW * 64, 0, stream>>>(a);                  \
+  } while (0)
+  const bool sq = a.dqd.splits > 1, sk = a.dkv.splits > 1;
+  if (a.dqd.nw == 1) XATTN_BWD(xattn_dq_kernel, 1, sq, gq);
+  else if (a.dqd.nw == 2) XATTN_BWD(xattn_dq_kernel, 2, sq, gq);
+  else XATTN_BWD(xattn_dq_kernel, 4, sq, gq);
+  if (a.dkv.nw == 1) XATTN_BWD(xattn_dkv_kernel, 1, sk, gk);
+  else if (a.dkv.nw == 2) XATTN_BWD(xattn_dkv_kernel, 2, sk, gk);
+  else XATTN_BWD(xattn_dkv_kernel, 4, sk, gk);
+#undef XATTN_BWD
+  if (sq) {
+    const XattnSum x{{a.part_dq, nullptr}, {a.dq, nullptr}, {a.ldq, a.ldq}, a.dqd.splits, a.H, a.Nq, all};
+    xattn_sum_kernel<<<dim3((unsigned)((all + 7) / 8), 1), 256, 0, stream>>>(x);
+  }
+  if (sk) {
+    const long long keys = (long long)a.B * a.G * a.Nk;
+    const XattnSum x{{a.part_dk, a.part_dv}, {a.dk, a.dv}, {a.ldk, a.ldv}, a.dkv.splits, a.G, a.Nk, keys};
+    xattn_sum_kernel<<<dim3((unsigned)((keys + 7) / 8), 2), 256, 0, stream>>>(x);
+  }
+}
+
+}  // namespace sla

@@ -1,0 +1,142 @@
+"""The operators of a DiT block together, as a program strings them up: at inference around the low-bit attention and the W8A8
+layers, eagerly and as one captured graph; in training with the gradients all the way back."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_oracle as bo
+from oracle import w8a8_oracle as wo
+from paper_2512_16093_amd import binding as sla
+
+pytestmark = pytest.mark.gpu
+H, D = 2, 128
+K = H * D
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _bf16(r, shape, amp=1.0):
+    return torch.from_numpy((amp * r.standard_normal(shape)).astype(np.float32)).bfloat16().cuda()
+
+
+def _rel(got, want):
+    return float(np.linalg.norm(_np(got) - want) / np.linalg.norm(want))
+
+
+class _Block:
+    """Self-attention (SLA), cross attention to a prompt, feed-forward up; token-major between the parts."""
+
+    def __init__(self, grid, prompt, seed):
+        r = np.random.default_rng(seed)
+        self.N = grid[0] * grid[1] * grid[2]
+        n = torch.arange(self.N)
+        self.pos = torch.stack((n // (grid[1] * grid[2]), n // grid[2] % grid[1], n % grid[2]), 1).int().cuda()
+        self.plan = sla.rope_make_plan()
+        weight = lambda rows: sla.w8a8_quantize_weight(_bf16(r, (rows, K), K ** -0.5))
+        self.w_qkv, self.w_out, self.w_q, self.w_o, self.w_up = weight(3 * K), weight(K), weight(K), weight(K), weight(512)
+        self.n1, self.n2, self.n3, self.qn, self.kn = ((1 + 0.2 * _bf16(r, K)).bfloat16() for _ in range(5))
+        self.states = [_bf16(r, (1, prompt, H, D), a).permute(0, 2, 1, 3) for a in (1.5, 1.0)]
+        self.lens = torch.tensor([prompt - 5], dtype=torch.int32, device="cuda")
+
+    def heads(self, t):
+        return t.view(1, self.N, H, D).permute(0, 2, 1, 3)
+
+    def __call__(self, x):
+        """Everything that lies between the parts, by name."""
+        N, e = self.N, {"x": x}
+        e["qkv"], _ = sla.w8a8_norm_linear_fwd(x, self.n1, self.w_qkv, 3 * K)
+        q, k, v = (e["qkv"].view(1, N, 3, H, D)[:, :, i].permute(0, 2, 1, 3) for i in range(3))
+        e["q"], e["k"] = sla.rope_qk_fwd(q, k, self.pos, self.plan, self.qn, self.kn, "token")
+        e["att"] = torch.empty((N, K), dtype=torch.bfloat16, device="cuda")
+        sla.sla_attention_fwd_strided(e["q"], e["k"], v, self.heads(e["att"]), 64, 64, 0.3, 0.3)
+        e["att_out"] = sla.w8a8_linear_fwd(e["att"], self.w_out, K)
+        e["cq"], e["h1"] = sla.w8a8_norm_linear_fwd(x, self.n2, self.w_q, K, res=e["att_out"])
+        e["cross"] = torch.empty((N, K), dtype=torch.bfloat16, device="cuda")
+        sla.xattn_fwd(self.heads(e["cq"]), *self.states, k_lens=self.lens, out=self.heads(e["cross"]))
+        e["cross_out"] = sla.w8a8_linear_fwd(e["cross"], self.w_o, K)
+        e["up"], e["h2"] = sla.w8a8_norm_linear_fwd(e["h1"], self.n3, self.w_up, 512, res=e["cross_out"])
+        return e
+
+
+@pytest.mark.parametrize("grid,prompt", [((3, 9, 11), 77), ((1, 1, 1), 6), ((2, 16, 16), 300)])
+def test_inference_chain(grid, prompt):
+    """Each part against float64 on what the part before left: bf16 results, off by 2^-8 of the terms at most, by less than half
+    of that in the mean; the W8A8 products by the codes that other roundings flip (a step is 1 / 127 of a block's largest value; 1 %)."""
+    blk = _Block(grid, prompt, [1, *grid])
+    x = _bf16(np.random.default_rng(7), (blk.N, K), 2.0)
+    e = blk(x)
+    e64 = {n: _np(t) for n, t in e.items()}
+    plain = lambda h, w, wq, rows: _linear(bo.norm_fwd(h, _np(w), 1e-6), wq, rows)
+
+    def _linear(n, wq, rows):
+        codes, scales = [_np(t) for t in sla.w8a8_debug_unpack(wq, True, rows, K)]
+        weight = codes * np.repeat(np.repeat(scales, 128, 0), 128, 1)
+        c, s = wo.quantize_blocks(n)
+        return (c * np.repeat(np.repeat(s, 128, 0), 128, 1)[:n.shape[0]]) @ weight.T
+    assert _rel(e["qkv"], plain(e64["x"], blk.n1, blk.w_qkv, 3 * K)) < 1e-2
+    qkv = e64["qkv"].reshape(1, blk.N, 3, H, D).transpose(2, 0, 3, 1, 4)
+    ang = bo.angles(blk.pos.cpu().numpy()[None], (22, 21, 21), (10000.0,) * 3)
+    for i, (name, w) in enumerate((("q", blk.qn), ("k", blk.kn))):
+        assert _rel(e[name], bo.rope_fwd(qkv[i], ang, "interleaved", _np(w), "token")) < 2 ** -9
+    v = e["qkv"].view(1, blk.N, 3, H, D)[:, :, 2].permute(0, 2, 1, 3)
+    same = sla.sla_attention_fwd(e["q"], e["k"], v.contiguous(), 64, 64, 0.3, 0.3)
+    assert torch.equal(same, blk.heads(e["att"]))
+    assert torch.equal(e["h1"].cpu(), (x.float() + e["att_out"].float()).bfloat16().cpu())
+    assert _rel(e["cq"], plain(e64["h1"], blk.n2, blk.w_q, K)) < 1e-2
+    cross = bo.xattn_fwd(_np(blk.heads(e["cq"])), _np(blk.states[0]), _np(blk.states[1]), [prompt - 5])[0]
+    assert _rel(blk.heads(e["cross"]), cross) < 2 ** -8
+    assert _rel(e["up"], plain(e64["h2"], blk.n3, blk.w_up, 512)) < 1e-2
+    # the whole block as one graph, replayed on new inputs with eager work between
+    held_x = x.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = blk(held_x)
+    for seed in range(3):
+        held_x.copy_(_bf16(np.random.default_rng([8, seed]), (blk.N, K), 2.0))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = {n: t.clone() for n, t in held.items()}
+        eager = blk(held_x.clone())
+        assert all(torch.equal(replayed[n], eager[n]) for n in eager), seed
+
+
+@pytest.mark.parametrize("N,Nk,groups", [(50, 20, 2), (300, 77, 1)])
+def test_training_chain(N, Nk, groups):
+    """Norm, rotation and cross attention one after the other, and back: against the chain rule in float64 on the formulas.  Eight
+    roundings to bf16 lie on the way to each gradient, off by 2^-9 in the mean at most each."""
+    r = np.random.default_rng([N, Nk])
+    x, res, dout = _bf16(r, (N, K)), _bf16(r, (N, K), 0.3), _bf16(r, (1, H, N, D), 0.1)
+    mem_k, mem_v = (_bf16(r, (1, H // groups, Nk, D), 1.5) for _ in range(2))
+    w, qw, kw = (1 + 0.2 * _bf16(r, K)).bfloat16(), (1 + 0.2 * _bf16(r, K)).bfloat16(), (1 + 0.2 * _bf16(r, D)).bfloat16()
+    pos_q, pos_k = (torch.from_numpy(r.integers(0, 60, (n, 3)).astype(np.int32)).cuda() for n in (N, Nk))
+    plan = sla.rope_make_plan()
+    heads = lambda t: t.view(1, N, H, D).permute(0, 2, 1, 3)
+
+    y, h = sla.norm_rms_fwd(x, w, res)
+    q, _ = sla.rope_qk_fwd(heads(y), None, pos_q, plan, qw, None, "token")
+    k, _ = sla.rope_qk_fwd(mem_k, None, pos_k, plan, kw, None, "head")
+    out, lse = sla.xattn_fwd(q, k, mem_v, want_lse=True)
+    dq, dk, dv = sla.xattn_bwd(q, k, mem_v, out, dout, lse)
+    d_mem, _, dkw, _ = sla.rope_qk_bwd(dk, None, pos_k, plan, mem_k, None, kw, None, "head")
+    dy = torch.empty((N, K), dtype=torch.bfloat16, device="cuda")
+    _, _, dqw, _ = sla.rope_qk_bwd(dq, None, pos_q, plan, heads(y), None, qw, None, "token", dq=heads(dy))
+    dx, dw = sla.norm_rms_bwd(dy, h, w)
+
+    leaves = [t.detach().double().cpu().requires_grad_() for t in (h, w, mem_k, mem_v, qw, kw)]
+    h64, w64, mk, mv, qw64, kw64 = leaves
+
+    def turned(t, pos):
+        ang = torch.from_numpy(bo.angles(pos.cpu().numpy(), (22, 21, 21), (10000.0,) * 3))
+        lo, hi = t[..., 0::2], t[..., 1::2]
+        return torch.stack((lo * ang.cos() - hi * ang.sin(), lo * ang.sin() + hi * ang.cos()), -1).flatten(-2)
+    rms = lambda t, dims: t * torch.rsqrt((t * t).mean(dims, keepdim=True) + 1e-6)
+    y64 = rms(h64, 1) * w64
+    q64 = turned(rms(heads(y64), (1, 3)) * qw64.view(1, H, 1, D), pos_q)
+    k64 = turned(rms(mk, 3) * kw64, pos_k).repeat_interleave(groups, 1)
+    out64 = torch.softmax(q64 @ k64.transpose(2, 3) * D ** -0.5, 3) @ mv.repeat_interleave(groups, 1)
+    (out64 * dout.double().cpu()).sum().backward()
+    assert _rel(out, out64.detach().numpy()) < 8 * 2 ** -9
+    for name, got, leaf in zip(("dx", "dw", "d mem_k", "dv", "dq weight", "dk weight"), (dx, dw, d_mem, dv, dqw, dkw), leaves):
+        assert _rel(got, leaf.grad.numpy()) < 8 * 2 ** -9, (name, _rel(got, leaf.grad.numpy()))

@@ -21,7 +21,7 @@ def _declared(header, prefix):
     return set(re.findall(r"\b(%s_[a-z0-9_]+)\s*\(" % prefix, text))
 
 
-@pytest.mark.parametrize("prefix,names", [("rope", sla.ROPE_EXPORTS), ("norm", sla.NORM_EXPORTS)])
+@pytest.mark.parametrize("prefix,names", [("rope", sla.ROPE_EXPORTS), ("norm", sla.NORM_EXPORTS), ("xattn", sla.XATTN_EXPORTS)])
 def test_library_exports_every_declared_symbol(prefix, names):
     assert _declared(prefix + ".h", prefix) == set(names)
     for n in names:
@@ -154,6 +154,47 @@ def test_norm_linear_argument_errors():
     assert linear(y=ODD) == sla.ERR_LAYOUT and linear(bias=ctypes.c_void_p(0x1004)) == sla.ERR_LAYOUT
 
 
+def test_xattn_argument_errors():
+    L = sla.lib()
+    need, need_b = sla.xattn_workspace_bytes(1, 40, 10, 1, 8192, 128), sla.xattn_bwd_workspace_bytes(1, 40, 10, 1, 8192, 128)
+    assert need > 2 * 40 * 128 * 4 and need_b > 2 * 40 * 128 * 4                     # few queries: pieces of the walk over the keys
+    assert sla.xattn_workspace_bytes(1, 40, 40, 75600, 512, 128) == 256
+    shapes = (dict(B=0), dict(H=0), dict(Hkv=0), dict(Nq=0), dict(Nk=0), dict(d=64), dict(H=40, Hkv=12), dict(B=65536, H=1, Hkv=1),
+              dict(H=64, Hkv=64, Nq=1 << 24), dict(H=64, Hkv=64, Nk=1 << 24))
+    strides = (sla.Strides(0, 0, 64), sla.Strides(0, 132, 256), sla.Strides(-8, 128, 256))
+
+    def fwd(q=FAKE, k=FAKE, v=FAKE, out=FAKE, lse=None, qs=None, vs=None, lens=None, B=1, H=40, Hkv=10, Nq=1, Nk=8192, d=128, scale=0.0,
+            ws=WS, wsb=BIG):
+        return L.xattn_fwd(q, k, v, out, lse, qs, None, vs, None, lens, B, H, Hkv, Nq, Nk, d, scale, ws, wsb, None)
+
+    def bwd(s=None, lens=None, B=1, H=40, Hkv=10, Nq=1, Nk=8192, d=128, scale=0.0, ws=WS, wsb=BIG, **kw):
+        p = [kw.get(n, FAKE) for n in ("q", "k", "v", "out", "dout", "lse", "dq", "dk", "dv")]
+        return L.xattn_bwd(*p, s, lens, B, H, Hkv, Nq, Nk, d, scale, ws, wsb, None)
+
+    for n in ("q", "k", "v", "out"):
+        assert fwd(**{n: None}) == sla.ERR_NULL and fwd(**{n: ODD}) == sla.ERR_LAYOUT, n
+    for n in ("q", "k", "v", "out", "dout", "lse", "dq", "dk", "dv"):
+        assert bwd(**{n: None}) == sla.ERR_NULL, n
+        assert bwd(**{n: ODD if n != "lse" else ctypes.c_void_p(0x1002)}) == sla.ERR_LAYOUT, n
+    for call, bytes_ in ((fwd, need), (bwd, need_b)):
+        for kw in shapes:
+            assert call(**kw) == sla.ERR_SHAPE, kw
+        for bad in (-0.1, float("nan"), float("inf"), 1e-40):
+            assert call(scale=bad) == sla.ERR_VALUE
+        assert call(ws=None) == sla.ERR_WORKSPACE and call(wsb=bytes_ - 1) == sla.ERR_WORKSPACE
+        assert call(ws=ctypes.c_void_p(0x10010)) == sla.ERR_WORKSPACE
+        assert call(lens=ctypes.c_void_p(0x1002)) == sla.ERR_LAYOUT
+    for bad in strides:
+        assert fwd(qs=ctypes.byref(bad)) == sla.ERR_LAYOUT and fwd(vs=ctypes.byref(bad)) == sla.ERR_LAYOUT
+        for i in range(8):
+            each = [None] * 8
+            each[i] = ctypes.pointer(bad)
+            assert bwd(s=ctypes.byref(sla.XattnBwdStrides(*each))) == sla.ERR_LAYOUT
+    for kw in shapes:
+        a = dict(dict(B=1, H=40, Hkv=10, Nq=1, Nk=8192, d=128), **kw)
+        assert sla.xattn_workspace_bytes(**a) == 0 and sla.xattn_bwd_workspace_bytes(**a) == 0
+
+
 def test_binding_refuses_wrong_tensors():
     x = torch.zeros((1, 2, 64, 128), dtype=torch.bfloat16)      # CPU tensors
     m = torch.zeros((4, 128), dtype=torch.bfloat16)
@@ -161,6 +202,7 @@ def test_binding_refuses_wrong_tensors():
     for call in (lambda: sla.rope_qk_fwd(x, x, pos, plan), lambda: sla.rope_qk_bwd(x, x, pos, plan),
                  lambda: sla.rope_qk_fwd(x, x, pos, plan, norm="row"), lambda: sla.norm_rms_fwd(m, None),
                  lambda: sla.norm_rms_bwd(m, m, None), lambda: sla.w8a8_norm_quantize_act(m, None),
-                 lambda: sla.w8a8_norm_linear_fwd(m, None, m, 128)):
+                 lambda: sla.w8a8_norm_linear_fwd(m, None, m, 128), lambda: sla.xattn_fwd(x, x, x), lambda: sla.xattn_fwd(x, x, x, scale=-1.0),
+                 lambda: sla.xattn_bwd(x, x, x, x, x, torch.zeros(128))):
         with pytest.raises(ValueError):
             call()
