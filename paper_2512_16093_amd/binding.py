@@ -616,25 +616,28 @@ def sla_fwd_attend(q, out, block_q, block_k, topk_ratio, marginal_ratio, workspa
 # ---------------------------------------------------------------------------
 # include/rope.h, include/norm.h and the norm in front of a W8A8 layer
 # ---------------------------------------------------------------------------
-class _on:
-    """Makes the device of `t` the current one for a call, so that the launch and its stream are that device's; every
-    other tensor of the call has to lie there."""
+# These calls are short (a kernel or two of a few microseconds), so their marshalling is kept short as well: addresses are
+# passed as plain integers, layouts only where a tensor is not contiguous, the stream without an object around it.
+def _launch(name, device, tensors, *args):
+    """Calls the C entry point `name` with args and the current stream of `device`, made the current device where it is not;
+    every one of `tensors` has to lie there."""
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("%s: expected CUDA tensors of one device" % name)
+    if device.type != "cuda":
+        raise ValueError("%s: expected CUDA tensors" % name)
+    f = getattr(lib(), name)
+    if device.index == torch.cuda.current_device():
+        st = f(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    else:
+        with torch.cuda.device(device):
+            st = f(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if st != SLA_OK:
+        raise SLAError(st, name)
 
-    def __init__(self, t, *others):
-        if not t.is_cuda:
-            raise ValueError("expected CUDA tensors")
-        for o in others:
-            if o is not None and o.device != t.device:
-                raise ValueError("the tensors of a call have to lie on one device")
-        self.other = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
 
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-
-    def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def _rows_of(t, what, shape=None):
@@ -699,12 +702,28 @@ def _heads_like(x):
     return torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
 
 
-def _strides_or_none(t, what, like):
+def _layout(t, what, like):
+    """The strides of a tensor indexed [B,heads,N,d], shaped like `like`; None where the library's own assumption holds."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(like.shape):
-        raise ValueError("%s: expected the shape %r" % (what, tuple(like.shape)))
-    return ctypes.pointer(_strides_of(t, what))
+    if t.shape != like.shape or t.dtype != torch.bfloat16:
+        raise ValueError("%s: expected a bfloat16 tensor of %r" % (what, tuple(like.shape)))
+    if t.is_contiguous():
+        return None
+    sb, sh, sn, sc = t.stride()
+    B, H, N, d = t.shape
+    if sc != 1 and d != 1:
+        raise ValueError("%s: expected contiguous channels" % what)
+    # (the stride of an index that has one value says nothing)
+    return Strides(sb if B > 1 else 0, sh if H > 1 else 0, sn if N > 1 else d)
+
+
+def _by_ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def _pointers(struct, layouts):
+    return None if not any(layouts) else ctypes.byref(struct(*[None if s is None else ctypes.pointer(s) for s in layouts]))
 
 
 def rope_qk_fwd(q, k, positions, plan, q_weight=None, k_weight=None, norm="none", eps=1e-6, q_out=None, k_out=None):
@@ -713,11 +732,10 @@ def rope_qk_fwd(q, k, positions, plan, q_weight=None, k_weight=None, norm="none"
     B, H, Hk, N, d, pb, kind = _rope_args(q, k, positions, norm, q_weight, k_weight)
     q_out = _heads_like(q) if q_out is None else q_out
     k_out = _heads_like(k) if k_out is None and k is not None else k_out
-    s = [_strides_or_none(t, n, like) for t, n, like in ((q, "q", q), (k, "k", k), (q_out, "q_out", q), (k_out, "k_out", k))]
-    with _on(q, k, q_out, k_out, positions, q_weight, k_weight):
-        st = lib().rope_qk_fwd(_ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), *s, _ptr(positions), pb, _ptr(q_weight),
-                               _ptr(k_weight), kind, eps, B, H, Hk, N, d, ctypes.byref(plan), _stream())
-    _check(st, "rope_qk_fwd")
+    _launch("rope_qk_fwd", q.device, (k, q_out, k_out, positions, q_weight, k_weight), _at(q), _at(k), _at(q_out), _at(k_out),
+            _by_ref(_layout(q, "q", q)), _by_ref(_layout(k, "k", k)), _by_ref(_layout(q_out, "q_out", q)),
+            _by_ref(_layout(k_out, "k_out", k)), _at(positions), pb, _at(q_weight), _at(k_weight), kind, eps, B, H, Hk, N, d,
+            ctypes.byref(plan))
     return q_out, k_out
 
 
@@ -734,20 +752,18 @@ def rope_qk_bwd(dq_out, dk_out, positions, plan, q=None, k=None, q_weight=None, 
         q = k = q_weight = k_weight = None
     dq = _heads_like(dq_out) if dq is None else dq
     dk = _heads_like(dk_out) if dk is None and dk_out is not None else dk
-    named = ((dq_out, "dq_out", dq_out), (dk_out, "dk_out", dk_out), (q, "q", dq_out), (k, "k", dk_out), (dq, "dq", dq_out),
-             (dk, "dk", dk_out))
-    s = RopeBwdStrides(*[_strides_or_none(*x) for x in named])
+    s = [_layout(*x) for x in ((dq_out, "dq_out", dq_out), (dk_out, "dk_out", dk_out), (q, "q", dq_out), (k, "k", dk_out),
+                               (dq, "dq", dq_out), (dk, "dk", dk_out))]
     dqw = dkw = None
     if want_dw and norm != "none":
         dqw = torch.empty(d if norm == "head" else H * d, dtype=torch.float32, device=dq_out.device)
         if dk_out is not None:
             dkw = torch.empty(d if norm == "head" else Hk * d, dtype=torch.float32, device=dq_out.device)
         workspace = _scratch(workspace, lib().rope_bwd_workspace_bytes(B, H, Hk, N, d, kind), dq_out.device, "rope_qk_bwd")
-    with _on(dq_out, dk_out, q, k, dq, dk, positions, q_weight, k_weight, workspace):
-        st = lib().rope_qk_bwd(_ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(dq), _ptr(dk), _ptr(dqw), _ptr(dkw),
-                               ctypes.byref(s), _ptr(positions), pb, _ptr(q_weight), _ptr(k_weight), kind, eps, B, H, Hk, N, d,
-                               ctypes.byref(plan), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
-    _check(st, "rope_qk_bwd")
+    _launch("rope_qk_bwd", dq_out.device, (dk_out, q, k, dq, dk, positions, q_weight, k_weight, workspace), _at(dq_out), _at(dk_out),
+            _at(q), _at(k), _at(dq), _at(dk), _at(dqw), _at(dkw), _pointers(RopeBwdStrides, s), _at(positions), pb, _at(q_weight),
+            _at(k_weight), kind, eps, B, H, Hk, N, d, ctypes.byref(plan), _at(workspace),
+            0 if workspace is None else workspace.numel())
     return dq, dk, dqw, dkw
 
 
@@ -763,9 +779,7 @@ def norm_rms_fwd(x, w, res=None, eps=1e-6, out=None, h=None):
         _rows_of(h, "h", (M, K))
     elif h is not None:
         raise ValueError("h is written only where there is a res")
-    with _on(x, w, res, out, h):
-        st = lib().norm_rms_fwd(_ptr(x), _ptr(res), _ptr(w), _ptr(h), _ptr(out), M, K, eps, _stream())
-    _check(st, "norm_rms_fwd")
+    _launch("norm_rms_fwd", x.device, (w, res, out, h), _at(x), _at(res), _at(w), _at(h), _at(out), M, K, eps)
     return out, x if res is None else h
 
 
@@ -786,10 +800,8 @@ def norm_rms_bwd(dy, h, w, dh=None, eps=1e-6, dx=None, want_dw=True, workspace=N
     if want_dw:
         dw = torch.empty(K, dtype=torch.float32, device=dy.device)
         workspace = _scratch(workspace, norm_bwd_workspace_bytes(M, K), dy.device, "norm_rms_bwd")
-    with _on(dy, h, w, dh, dx, workspace):
-        st = lib().norm_rms_bwd(_ptr(dy), _ptr(dh), _ptr(h), _ptr(w), _ptr(dx), _ptr(dw), M, K, eps, _ptr(workspace),
-                                0 if workspace is None else workspace.numel(), _stream())
-    _check(st, "norm_rms_bwd")
+    _launch("norm_rms_bwd", dy.device, (h, w, dh, dx, workspace), _at(dy), _at(dh), _at(h), _at(w), _at(dx), _at(dw), M, K, eps,
+            _at(workspace), 0 if workspace is None else workspace.numel())
     return dx, dw
 
 
@@ -812,10 +824,8 @@ def _w8a8_norm_args(x, norm_w, res, h, workspace, where):
 def w8a8_norm_quantize_act(x, norm_w, res=None, eps=1e-6, h=None, workspace=None):
     """(workspace, h): a workspace for w8a8_gemm_fwd holding the quantised norm of h = x + res (x itself without res)."""
     M, K, h, workspace = _w8a8_norm_args(x, norm_w, res, h, workspace, "w8a8_norm_quantize_act")
-    with _on(x, norm_w, res, h, workspace):
-        st = lib().w8a8_norm_quantize_act(_ptr(x), _ptr(res), _ptr(norm_w), _ptr(h), M, K, eps, _ptr(workspace),
-                                          workspace.numel(), _stream())
-    _check(st, "w8a8_norm_quantize_act")
+    _launch("w8a8_norm_quantize_act", x.device, (norm_w, res, h, workspace), _at(x), _at(res), _at(norm_w), _at(h), M, K, eps,
+            _at(workspace), workspace.numel())
     return workspace, x if res is None else h
 
 
@@ -828,10 +838,8 @@ def w8a8_norm_linear_fwd(x, norm_w, wq, N, res=None, eps=1e-6, bias=None, worksp
         raise ValueError("wq: expected the weight object of an [%d, %d] weight" % (N, K))
     out = torch.empty((M, N), dtype=torch.bfloat16, device=x.device) if out is None else out
     _rows_of(out, "out", (M, N))
-    with _on(x, norm_w, res, h, wq, bias, out, workspace):
-        st = lib().w8a8_norm_linear_fwd(_ptr(x), _ptr(res), _ptr(norm_w), _ptr(h), _ptr(wq), _ptr(bias), _ptr(out), M, N, K, eps,
-                                        _ptr(workspace), workspace.numel(), _stream())
-    _check(st, "w8a8_norm_linear_fwd")
+    _launch("w8a8_norm_linear_fwd", x.device, (norm_w, res, h, wq, bias, out, workspace), _at(x), _at(res), _at(norm_w), _at(h), _at(wq),
+            _at(bias), _at(out), M, N, K, eps, _at(workspace), workspace.numel())
     return out, x if res is None else h
 
 
@@ -863,12 +871,10 @@ def xattn_fwd(q, k, v, k_lens=None, scale=None, out=None, want_lse=False, worksp
     dims, scale = _xattn_args(q, k, v, k_lens, scale)
     out = _heads_like(q) if out is None else out
     lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
-    s = [_strides_or_none(t, n, like) for t, n, like in ((q, "q", q), (k, "k", k), (v, "v", k), (out, "out", q))]
     workspace = _scratch(workspace, lib().xattn_workspace_bytes(*dims), q.device, "xattn_fwd")
-    with _on(q, k, v, out, k_lens, workspace):
-        st = lib().xattn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), *s, _ptr(k_lens), *dims, scale, _ptr(workspace),
-                             workspace.numel(), _stream())
-    _check(st, "xattn_fwd")
+    _launch("xattn_fwd", q.device, (k, v, out, k_lens, workspace), _at(q), _at(k), _at(v), _at(out), _at(lse),
+            _by_ref(_layout(q, "q", q)), _by_ref(_layout(k, "k", k)), _by_ref(_layout(v, "v", k)), _by_ref(_layout(out, "out", q)),
+            _at(k_lens), *dims, scale, _at(workspace), workspace.numel())
     return out, lse
 
 
@@ -877,11 +883,10 @@ def xattn_bwd(q, k, v, out, dout, lse, k_lens=None, scale=None, grads=None, work
     dims, scale = _xattn_args(q, k, v, k_lens, scale)
     _vector(lse, "lse", dims[0] * dims[1] * dims[3], torch.float32)
     dq, dk, dv = (_heads_like(t) for t in (q, k, k)) if grads is None else grads
-    named = ((q, "q", q), (k, "k", k), (v, "v", k), (out, "out", q), (dout, "dout", q), (dq, "dq", q), (dk, "dk", k), (dv, "dv", k))
-    s = XattnBwdStrides(*[_strides_or_none(*x) for x in named])
+    s = [_layout(*x) for x in ((q, "q", q), (k, "k", k), (v, "v", k), (out, "out", q), (dout, "dout", q), (dq, "dq", q), (dk, "dk", k),
+                               (dv, "dv", k))]
     workspace = _scratch(workspace, lib().xattn_bwd_workspace_bytes(*dims), q.device, "xattn_bwd")
-    with _on(q, k, v, out, dout, lse, dq, dk, dv, k_lens, workspace):
-        st = lib().xattn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(dout), _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv),
-                             ctypes.byref(s), _ptr(k_lens), *dims, scale, _ptr(workspace), workspace.numel(), _stream())
-    _check(st, "xattn_bwd")
+    _launch("xattn_bwd", q.device, (k, v, out, dout, lse, dq, dk, dv, k_lens, workspace), _at(q), _at(k), _at(v), _at(out), _at(dout),
+            _at(lse), _at(dq), _at(dk), _at(dv), _pointers(XattnBwdStrides, s), _at(k_lens), *dims, scale, _at(workspace),
+            workspace.numel())
     return dq, dk, dv

@@ -42,7 +42,7 @@ size_t bwd_map(XattnArgs* a, unsigned char* base) {
   size_t o = 0;
   auto take = [&](size_t floats) { float* p = (float*)(base + o); o += align256(4 * floats); return p; };
   a->lse2 = take(padded);
-  a->delta = take(padded);
+  a->neg_delta = take(padded);
   if (a->dqd.splits > 1) a->part_dq = take(a->dqd.splits * rows * D);
   if (a->dkv.splits > 1) {
     a->part_dk = take(a->dkv.splits * keys * D);

@@ -2,8 +2,7 @@
 //
 //   xattn_fwd_kernel     per 32 to 128 query rows, over the keys: one pass with a running maximum and sum.
 //   xattn_join_kernel    joins the pieces of a walk that was split: weights 2^(m - max m), one division.
-//   xattn_delta_kernel   delta = dout . out and the base-2 log-sum-exp, padded to whole steps of the dk, dv walk.
-//   xattn_dq_kernel      per 32 to 128 query rows, over the keys: dQ += dS K.
+//   xattn_dq_kernel      per 32 to 128 query rows, over the keys: delta = dout . out, dQ += dS K; leaves delta for the next one.
 //   xattn_dkv_kernel     per 32 to 128 keys, over the query rows of every head that shares them: dV += P^T dO, dK += dS^T Q.
 //   xattn_sum_kernel     adds up the pieces of split walks of the two.
 //
@@ -22,14 +21,23 @@
 
 namespace sla {
 
-// Consecutive workgroups go to the eight XCDs in turn: each XCD gets a contiguous eighth of the units, so that the
-// workgroups on it at a time work on neighbouring ones (the same slice's keys).  False: no unit.
-__device__ __forceinline__ bool xattn_unit(long long units, long long& unit) {
-  const long long per = (units + 7) >> 3, slot = blockIdx.x >> 3;
-  unit = (blockIdx.x & 7) * per + slot;
-  return slot < per && unit < units;
+constexpr int XATTN_PIECES = 1024;             // most pieces of a walk
+
+// Consecutive workgroups go to the eight XCDs in turn: each XCD gets a contiguous eighth of every sample's units, so that the
+// workgroups on it at a time work on neighbouring ones (the same slice's keys), and samples of different lengths leave no
+// XCD idle (an eighth of all the units: prompts of 512 and 128 states, 12 heads x 32760 queries 226 us, half the XCDs done early;
+// now 187).  Samples of few units, which do not divide by eight, are taken together.  False: no unit.
+__host__ __device__ inline long long xattn_part(long long per_sample, int B) { return per_sample >= 64 ? per_sample : per_sample * B; }
+__device__ __forceinline__ bool xattn_unit(long long per_sample, int B, long long& unit) {
+  const long long part = xattn_part(per_sample, B), per = (part + 7) >> 3, slot = blockIdx.x >> 3, which = slot / per;
+  const long long in_part = (blockIdx.x & 7) * per + (slot - which * per);
+  unit = which * part + in_part;
+  return in_part < part && unit < per_sample * B;
 }
-static unsigned xattn_grid(long long units) { return (unsigned)(8 * ((units + 7) / 8)); }
+static unsigned xattn_grid(long long per_sample, int B) {
+  const long long part = xattn_part(per_sample, B);
+  return (unsigned)(8 * ((part + 7) / 8) * (per_sample * B / part));
+}
 
 __device__ __forceinline__ int xattn_len(const XattnArgs& a, int b) {
   return a.lens ? min(max(__builtin_amdgcn_readfirstlane(a.lens[b]), 0), a.Nk) : a.Nk;
@@ -86,7 +94,7 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_fwd_kernel(XattnArgs a) {
   constexpr int KT = NW == 4 ? 2 : 1, STEP_B = 2 * KT * SWZ_TILE_B, STEP = 32 * KT;
   __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];   // two steps' tiles: KT of K, then KT of V
   long long unit;
-  if (!xattn_unit((long long)a.B * a.G * a.fwd.splits * a.fwd.tiles, unit)) return;
+  if (!xattn_unit((long long)a.G * a.fwd.splits * a.fwd.tiles, a.B, unit)) return;
   const int tile = (int)(unit % a.fwd.tiles), rest = (int)(unit / a.fwd.tiles);
   const int split = SPLIT ? rest % a.fwd.splits : 0, bg = SPLIT ? rest / a.fwd.splits : rest;
   const int b = bg / a.G, g = bg - b * a.G;
@@ -209,83 +217,91 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_fwd_kernel(XattnArgs a) {
   }
 }
 
-// Eight rows per workgroup, half a wavefront each; or (WIDE) one row, its pieces dealt to the eight halves.
+// One row per workgroup (or eight, half a wavefront each, where there are few pieces: !WIDE).  The pieces' maxima and sums are
+// read side by side, a lane each, and leave their weights 2^(m - max m) in LDS; then the pieces' rows are added up, dealt to
+// the eight halves of wavefronts (WIDE).  With the maxima read one after the other by every thread, 118 pieces took 28 us.
 template <bool WIDE>
 __global__ void __launch_bounds__(256) xattn_join_kernel(XattnArgs a) {
+  __shared__ float weight[WIDE ? XATTN_PIECES : 1];
   __shared__ float4 red_o[8][32];
-  __shared__ float2 red_l[8];
-  const int t = threadIdx.x, half = t >> 5, c = t & 31;
-  const long long all = (long long)a.B * a.H * a.Nq, row = WIDE ? blockIdx.x : 8ll * blockIdx.x + half;
-  if (row >= all) return;                      // (WIDE: of the whole workgroup)
+  __shared__ float red[3][4];
+  const int t = threadIdx.x, half = t >> 5, c = t & 31, lane = t & 63;
+  const long long all = (long long)a.B * a.H * a.Nq, row = WIDE ? blockIdx.x : min(8ll * blockIdx.x + half, all - 1);
   const int S = a.fwd.splits;
-  float M = -FLT_MAX;
-  for (int s = 0; s < S; ++s) {
-    const float4 ml = *(const float4*)(a.part_ml + 4 * (s * all + row));
-    if (ml.y > 0.f) M = fmaxf(M, ml.x);
-  }
+  float M = -FLT_MAX, l = 0.f, lx = 0.f;
   float4 o{0.f, 0.f, 0.f, 0.f};
-  float2 l{0.f, 0.f};
-#pragma unroll 4
-  for (int s = WIDE ? half : 0; s < S; s += WIDE ? 8 : 1) {
-    const float4 ml = *(const float4*)(a.part_ml + 4 * (s * all + row));
-    const float w = ml.y > 0.f ? __builtin_amdgcn_exp2f(ml.x - M) : 0.f;
+  auto piece = [&](int s, float w) __attribute__((always_inline)) {
+    // (a piece without keys has weight 0, and its row may hold anything finite: it was written as zeros)
     const float4 p = *(const float4*)(a.part_o + (s * all + row) * D + 4 * c);
     o.x = __builtin_fmaf(w, p.x, o.x); o.y = __builtin_fmaf(w, p.y, o.y);
     o.z = __builtin_fmaf(w, p.z, o.z); o.w = __builtin_fmaf(w, p.w, o.w);
-    l.x = __builtin_fmaf(w, ml.y, l.x);
-    l.y = __builtin_fmaf(w, ml.z, l.y);
-  }
+  };
   if constexpr (WIDE) {
+    float4 ml[XATTN_PIECES / 256];
+#pragma unroll
+    for (int u = 0; u < XATTN_PIECES / 256; ++u) {
+      const int s = t + 256 * u;
+      ml[u] = float4{-FLT_MAX, 0.f, 0.f, 0.f};
+      if (s < S) ml[u] = *(const float4*)(a.part_ml + 4 * (s * all + row));
+      M = fmaxf(M, ml[u].x);
+    }
+    M = rows_max(row_max(M));
+    if (lane == 0) red[0][t >> 6] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+#pragma unroll
+    for (int u = 0; u < XATTN_PIECES / 256; ++u) {
+      const float w = __builtin_amdgcn_exp2f(ml[u].x - M);
+      if (t + 256 * u < S) weight[t + 256 * u] = w;
+      l = __builtin_fmaf(w, ml[u].y, l);
+      lx = __builtin_fmaf(w, ml[u].z, lx);
+    }
+    l = rows_sum(row_sum(l));
+    lx = rows_sum(row_sum(lx));
+    if (lane == 0) { red[1][t >> 6] = l; red[2][t >> 6] = lx; }
+    __syncthreads();
+    l = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+    lx = red[2][0] + red[2][1] + red[2][2] + red[2][3];
+#pragma unroll 4
+    for (int s = half; s < S; s += 8) piece(s, weight[s]);
     red_o[half][c] = o;
-    if (c == 0) red_l[half] = l;
     __syncthreads();
     if (half != 0) return;
 #pragma unroll
     for (int i = 1; i < 8; ++i) {
       const float4 p = red_o[i][c];
       o.x += p.x; o.y += p.y; o.z += p.z; o.w += p.w;
-      l.x += red_l[i].x;
-      l.y += red_l[i].y;
     }
+  } else {
+    float4 ml[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      ml[s] = *(const float4*)(a.part_ml + 4 * (min(s, S - 1) * all + row));
+      M = fmaxf(M, ml[s].x);
+    }
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const float w = s < S ? __builtin_amdgcn_exp2f(ml[s].x - M) : 0.f;
+      l = __builtin_fmaf(w, ml[s].y, l);
+      lx = __builtin_fmaf(w, ml[s].z, lx);
+      if (s < S) piece(s, w);
+    }
+    if (8ll * blockIdx.x + half >= all) return;
   }
-  const float inv = l.x > 0.f ? 1.0f / l.x : 0.f;
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
   const long long bh = row / a.Nq;
   const int n = (int)(row - bh * a.Nq), b = (int)(bh / a.H), h = (int)(bh - (long long)b * a.H);
   *(uint2*)(a.out + b * a.lo.sb + h * a.lo.sh + n * a.lo.sn + 4 * c) = uint2{pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv)};
-  if (a.lse && c == 0) a.lse[row] = l.x > 0.f ? (M + __builtin_amdgcn_logf(l.y)) * LN2 : -INFINITY;
+  if (a.lse && c == 0) a.lse[row] = l > 0.f ? (M + __builtin_amdgcn_logf(lx)) * LN2 : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
-// Sixteen rows per workgroup, sixteen lanes each.  Rows that pad a head to whole steps, and rows without keys: lse = +infinity, so
-// that their weights are exactly zero.
-__global__ void __launch_bounds__(256) xattn_delta_kernel(XattnArgs a) {
-  const int padded = xattn_padded_rows(a.Nq), part = threadIdx.x & 15;
-  const long long i = 16ll * blockIdx.x + (threadIdx.x >> 4);
-  const long long bh = i / padded;
-  const int n = (int)(i - bh * padded), b = (int)(bh / a.H), h = (int)(bh - (long long)b * a.H);
-  float dot = 0.f, lse2 = INFINITY;
-  if (n < a.Nq) {
-    float x[8], y[8];
-    unpack8(*(const uint4*)(a.o + b * a.lo.sb + h * a.lo.sh + n * a.lo.sn + 8 * part), x);
-    unpack8(*(const uint4*)(a.dout + b * a.ldo.sb + h * a.ldo.sh + n * a.ldo.sn + 8 * part), y);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(x[e], y[e], dot);
-    const float l = a.lse_in[bh * a.Nq + n];
-    if (l > -INFINITY) lse2 = l * LOG2E;
-  }
-  dot = row_sum(dot);
-  if (part == 0) {
-    a.delta[i] = dot;
-    a.lse2[i] = lse2;
-  }
-}
-
 template <int NW, bool SPLIT>
 __global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
   constexpr int KT = NW == 4 ? 2 : 1, STEP_B = 2 * KT * SWZ_TILE_B, STEP = 32 * KT;
   __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];
   long long unit;
-  if (!xattn_unit((long long)a.B * a.G * a.dqd.splits * a.dqd.tiles, unit)) return;
+  if (!xattn_unit((long long)a.G * a.dqd.splits * a.dqd.tiles, a.B, unit)) return;
   const int tile = (int)(unit % a.dqd.tiles), rest = (int)(unit / a.dqd.tiles);
   const int split = SPLIT ? rest % a.dqd.splits : 0, bg = SPLIT ? rest / a.dqd.splits : rest;
   const int b = bg / a.G, g = bg - b * a.G;
@@ -300,12 +316,34 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
     uint4 qf[8], df[8];
     query_operands(a.q, QueryRows(a, a.lq, b, g), row, a.rows, hf, qf);
     query_operands(a.dout, QueryRows(a, a.ldo, b, g), row, a.rows, hf, df);
-    float lse2 = INFINITY, delta = 0.f;
-    if (row < a.rows) {
-      const int head = (unsigned)row / (unsigned)a.Nq;
-      const long long at = ((long long)b * a.H + g * a.group + head) * xattn_padded_rows(a.Nq) + (row - head * a.Nq);
-      lse2 = a.lse2[at];
-      delta = a.delta[at];
+    // The row's base-2 log-sum-exp and delta = dout . out, half of its channels in each lane of the pair; for the dk, dv kernel
+    // too, padded to whole steps of its walk (lse = +infinity: weights of exactly zero).
+    float lse2 = INFINITY, neg_delta = 0.f;
+    {
+      const bf16_t* o = a.o + QueryRows(a, a.lo, b, g).at(min(row, a.rows - 1));
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        float x[8], y[8];
+        unpack8(*(const uint4*)(o + 16 * ks + 8 * hf), x);
+        unpack8(df[ks], y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) neg_delta = __builtin_fmaf(-x[e], y[e], neg_delta);
+      }
+      neg_delta += partner_f32(neg_delta);
+      if (row < a.rows) {
+        const int head = (unsigned)row / (unsigned)a.Nq, n = row - head * a.Nq, padded = xattn_padded_rows(a.Nq);
+        const long long bh = (long long)b * a.H + g * a.group + head;
+        lse2 = a.lse_in[bh * a.Nq + n] * LOG2E;
+        if (hf == 0 && split == 0) {
+          a.lse2[bh * padded + n] = lse2;
+          a.neg_delta[bh * padded + n] = neg_delta;
+          if (n == a.Nq - 1)
+            for (int i = n + 1; i < padded; ++i) {
+              a.lse2[bh * padded + i] = INFINITY;
+              a.neg_delta[bh * padded + i] = 0.f;
+            }
+        }
+      }
     }
     TileCopy<NW> ck, cv;
     ck.init(a.k + b * a.lk.sb + g * a.lk.sh, a.lk.sn, w, lane);
@@ -331,7 +369,7 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
         const unsigned char *tk = ring + kt * SWZ_TILE_B, *tv = ring + (KT + kt) * SWZ_TILE_B;
         v16f s = v16f{}, dp;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] = -delta;
+        for (int r = 0; r < 16; ++r) dp[r] = neg_delta;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
           s = mfma_bf16(n_op_swz(tk, no, ks), qf[ks], s);
@@ -368,11 +406,11 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
 
 // A wavefront owns 32 keys and walks over the query rows of every head of its group, 32 QT rows a step.
 template <int NW, bool SPLIT>
-__global__ void __launch_bounds__(NW * 64, 1) xattn_dkv_kernel(XattnArgs a) {
-  constexpr int QT = 2, STEP_B = 2 * QT * SWZ_TILE_B + 512, STEP = 32 * QT;   // Q, dO, then lse2 and delta of the rows
+__global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) xattn_dkv_kernel(XattnArgs a) {
+  constexpr int QT = 2, STEP_B = 2 * QT * SWZ_TILE_B + 512, STEP = 32 * QT, DEEP = 2;  // Q, dO, then lse2 and -delta of the rows
   __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];
   long long unit;
-  if (!xattn_unit((long long)a.B * a.G * a.dkv.splits * a.dkv.tiles, unit)) return;
+  if (!xattn_unit((long long)a.G * a.dkv.splits * a.dkv.tiles, a.B, unit)) return;
   const int tile = (int)(unit % a.dkv.tiles), rest = (int)(unit / a.dkv.tiles);
   const int split = SPLIT ? rest % a.dkv.splits : 0, bg = SPLIT ? rest / a.dkv.splits : rest;
   const int b = bg / a.G, g = bg - b * a.G;
@@ -407,7 +445,7 @@ __global__ void __launch_bounds__(NW * 64, 1) xattn_dkv_kernel(XattnArgs a) {
       if (w == 0) {
         const long long at = stat0 + (long long)head * xattn_padded_rows(a.Nq) + row0;
         copy_floats(a.lse2 + at, 4u * lane, lds0 + half * STEP_B + 2 * QT * SWZ_TILE_B);
-        copy_floats(a.delta + at, 4u * lane, lds0 + half * STEP_B + 2 * QT * SWZ_TILE_B + 256);
+        copy_floats(a.neg_delta + at, 4u * lane, lds0 + half * STEP_B + 2 * QT * SWZ_TILE_B + 256);
       }
       if (++in_head == per_head) {
         in_head = 0;
@@ -424,36 +462,66 @@ __global__ void __launch_bounds__(NW * 64, 1) xattn_dkv_kernel(XattnArgs a) {
       const unsigned char* stat = ring + half * STEP_B + 2 * QT * SWZ_TILE_B + 16 * hf;
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
+        // The tile's 32 products take their operands from one stream of LDS reads, four ahead: Q and dO as rows (S, dP), then
+        // both transposed (dV, dK in turn).  Held to that order, the sums, the keys' operands and what is in flight fit 256
+        // registers: two wavefronts share a SIMD.
         const unsigned char *tq = ring + x * SWZ_TILE_B, *td = ring + (QT + x) * SWZ_TILE_B;
+        auto flip = [](int off, int bits) __attribute__((always_inline)) {   // (formed anew each time: sixteen addresses held would not fit)
+          int a;
+          asm volatile("v_xor_b32 %0, %2, %1" : "=v"(a) : "v"(off), "n"(bits));
+          return a;
+        };
+        auto operand = [&](int i) __attribute__((always_inline)) {
+          if (i < 16) return *(const uint4*)((i < 8 ? tq : td) + flip(no, (i & 7) << 5));
+          const int u = (i - 16) >> 3, ct = ((i - 16) >> 1) & 3;
+          const unsigned char* tile = (i & 1) ? tq : td;
+          union { v4s h[2]; uint4 v; } r;
+          r.h[0] = read_tr(tile + 16 * u * 256 + flip(to, ct << 6));
+          r.h[1] = read_tr(tile + (16 * u + 8) * 256 + flip(to, (ct << 6) ^ (2 << 4)));
+          return r.v;
+        };
+        uint4 op[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) op[i] = operand(i);
         v16f s = v16f{}, dp;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {          // (rows 8 u + 4 hf + 0..3 of the tile)
           const float4 d4 = *(const float4*)(stat + 256 + 128 * x + 32 * u);
-          dp[4 * u] = -d4.x; dp[4 * u + 1] = -d4.y; dp[4 * u + 2] = -d4.z; dp[4 * u + 3] = -d4.w;
+          dp[4 * u] = d4.x; dp[4 * u + 1] = d4.y; dp[4 * u + 2] = d4.z; dp[4 * u + 3] = d4.w;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          s = mfma_bf16(op[i % DEEP], kf[i], s);
+          op[i % DEEP] = operand(i + DEEP);
+          __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-          s = mfma_bf16(n_op_swz(tq, no, ks), kf[ks], s);
-          dp = mfma_bf16(n_op_swz(td, no, ks), vf[ks], dp);
+        for (int i = 8; i < 16; ++i) {         // behind a product: two exponentials
+          dp = mfma_bf16(op[i % DEEP], vf[i - 8], dp);
+          op[i % DEEP] = operand(i + DEEP);
+          const int e = 2 * (i - 8);
+          const float2 l2 = *(const float2*)(stat + 128 * x + 32 * (e >> 2) + 4 * (e & 3));
+          s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c2, -l2.x));
+          s[e + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], a.c2, -l2.y));
+          __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const float4 l4 = *(const float4*)(stat + 128 * x + 32 * u);
-          const float lr[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[4 * u + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * u + e], a.c2, -lr[e]));
-            dp[4 * u + e] *= s[4 * u + e];
-          }
-        }
+        uint4 pb[2], db[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const uint4 pb = acc_operand(s, u), db = acc_operand(dp, u);
+          pb[u] = acc_operand(s, u);
 #pragma unroll
-          for (int ct = 0; ct < 4; ++ct) {
-            dv[ct] = mfma_bf16(t_op_swz(td, to, ct, u), pb, dv[ct]);
-            dk[ct] = mfma_bf16(t_op_swz(tq, to, ct, u), db, dk[ct]);
-          }
+          for (int r = 8 * u; r < 8 * u + 8; ++r) dp[r] *= s[r];
+          db[u] = acc_operand(dp, u);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 16; i < 32; ++i) {
+          const int u = (i - 16) >> 3, ct = ((i - 16) >> 1) & 3;
+          if (i & 1) dk[ct] = mfma_bf16(op[i % DEEP], db[u], dk[ct]);
+          else dv[ct] = mfma_bf16(op[i % DEEP], pb[u], dv[ct]);
+          if (i + DEEP < 32) op[i % DEEP] = operand(i + DEEP);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
@@ -509,7 +577,7 @@ __global__ void __launch_bounds__(256) xattn_sum_kernel(XattnSum x) {
 static XattnDeal deal(long long units, int nw, int tiles, int walk, int step, int least, long long places) {
   // As many pieces as there are places for, none shorter than `least`.
   const long long most = std::max<long long>(1, walk / least), want = std::max<long long>(1, places / std::max<long long>(1, units));
-  const int pieces = (int)std::min(most, want);
+  const int pieces = (int)std::min(std::min(most, want), (long long)XATTN_PIECES);
   int chunk = (walk + pieces - 1) / pieces;
   chunk = (chunk + step - 1) / step * step;
   return XattnDeal{nw, tiles, (walk + chunk - 1) / chunk, chunk};
@@ -520,19 +588,19 @@ XattnDeal xattn_deal_rows(int B, int G, int rows, int Nk) {
 }
 XattnDeal xattn_deal_keys(int B, int G, int group, int Nq, int Nk) {
   const int nw = Nk <= 32 ? 1 : Nk <= 64 ? 2 : 4, tiles = (Nk + 32 * nw - 1) / (32 * nw);
-  return deal((long long)B * G * tiles, nw, tiles, group * ((Nq + 63) / 64), 1, 4, (long long)compute_units() * (nw == 4 ? 1 : 2));
+  return deal((long long)B * G * tiles, nw, tiles, group * ((Nq + 63) / 64), 1, 4, (long long)compute_units() * 2);
 }
 
 void launch_xattn_fwd(const XattnArgs& a, hipStream_t stream) {
-  const long long units = (long long)a.B * a.G * a.fwd.splits * a.fwd.tiles;
+  const unsigned grid = xattn_grid((long long)a.G * a.fwd.splits * a.fwd.tiles, a.B);
 #define XATTN_FWD(NW)                                                                                                          \
   do {                                                                                                                         \
     if (a.fwd.splits > 1) {                                                                                                    \
-      if (a.lse) xattn_fwd_kernel<NW, true, true><<<xattn_grid(units), NW * 64, 0, stream>>>(a);                               \
-      else xattn_fwd_kernel<NW, false, true><<<xattn_grid(units), NW * 64, 0, stream>>>(a);                                    \
+      if (a.lse) xattn_fwd_kernel<NW, true, true><<<grid, NW * 64, 0, stream>>>(a);                               \
+      else xattn_fwd_kernel<NW, false, true><<<grid, NW * 64, 0, stream>>>(a);                                    \
     } else {                                                                                                                   \
-      if (a.lse) xattn_fwd_kernel<NW, true, false><<<xattn_grid(units), NW * 64, 0, stream>>>(a);                              \
-      else xattn_fwd_kernel<NW, false, false><<<xattn_grid(units), NW * 64, 0, stream>>>(a);                                   \
+      if (a.lse) xattn_fwd_kernel<NW, true, false><<<grid, NW * 64, 0, stream>>>(a);                              \
+      else xattn_fwd_kernel<NW, false, false><<<grid, NW * 64, 0, stream>>>(a);                                   \
     }                                                                                                                          \
   } while (0)
   if (a.fwd.nw == 1) XATTN_FWD(1);
@@ -547,9 +615,8 @@ void launch_xattn_fwd(const XattnArgs& a, hipStream_t stream) {
 }
 
 void launch_xattn_bwd(const XattnArgs& a, hipStream_t stream) {
-  const long long all = (long long)a.B * a.H * a.Nq, padded = (long long)a.B * a.H * xattn_padded_rows(a.Nq);
-  xattn_delta_kernel<<<(unsigned)(padded / 16), 256, 0, stream>>>(a);
-  const unsigned gq = xattn_grid((long long)a.B * a.G * a.dqd.splits * a.dqd.tiles), gk = xattn_grid((long long)a.B * a.G * a.dkv.splits * a.dkv.tiles);
+  const long long all = (long long)a.B * a.H * a.Nq;
+  const unsigned gq = xattn_grid((long long)a.G * a.dqd.splits * a.dqd.tiles, a.B), gk = xattn_grid((long long)a.G * a.dkv.splits * a.dkv.tiles, a.B);
 #define XATTN_BWD(KERNEL, NW, SPLIT, GRID)                                    \
   do {                                                                        \
     if (SPLIT) KERNEL<NW, true><<<GRID, NW * 64, 0, stream>>>(a);             \

@@ -22,7 +22,7 @@ struct XattnArgs {
   XattnDeal fwd, dqd, dkv;
   // workspace
   float *part_o, *part_ml;              // forward: fp32 [splits, B H Nq, 128], [splits, B H Nq, 4]
-  float *lse2, *delta;                  // backward: fp32 [B H, padded_rows(Nq)]
+  float *lse2, *neg_delta;                 // backward: fp32 [B H, padded_rows(Nq)]
   float *part_dq, *part_dk, *part_dv;   // fp32 [splits, ...]
 };
 __host__ __device__ inline int xattn_padded_rows(int Nq) { return (Nq + 63) / 64 * 64; }

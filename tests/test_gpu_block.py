@@ -68,13 +68,12 @@ def test_inference_chain(grid, prompt):
     x = _bf16(np.random.default_rng(7), (blk.N, K), 2.0)
     e = blk(x)
     e64 = {n: _np(t) for n, t in e.items()}
-    plain = lambda h, w, wq, rows: _linear(bo.norm_fwd(h, _np(w), 1e-6), wq, rows)
 
-    def _linear(n, wq, rows):
+    def plain(h, w, wq, rows):
         codes, scales = [_np(t) for t in sla.w8a8_debug_unpack(wq, True, rows, K)]
-        weight = codes * np.repeat(np.repeat(scales, 128, 0), 128, 1)
-        c, s = wo.quantize_blocks(n)
-        return (c * np.repeat(np.repeat(s, 128, 0), 128, 1)[:n.shape[0]]) @ weight.T
+        n = wo.dequantize_blockwise(*wo.quantize_blockwise(bo.norm_fwd(h, _np(w), 1e-6)))
+        return n @ wo.dequantize_blockwise(codes, scales).T
+
     assert _rel(e["qkv"], plain(e64["x"], blk.n1, blk.w_qkv, 3 * K)) < 1e-2
     qkv = e64["qkv"].reshape(1, blk.N, 3, H, D).transpose(2, 0, 3, 1, 4)
     ang = bo.angles(blk.pos.cpu().numpy()[None], (22, 21, 21), (10000.0,) * 3)
