@@ -27,17 +27,44 @@ constexpr int XATTN_PIECES = 1024;             // most pieces of a walk
 // workgroups on it at a time work on neighbouring ones (the same slice's keys), and samples of different lengths leave no
 // XCD idle (an eighth of all the units: prompts of 512 and 128 states, 12 heads x 32760 queries 226 us, half the XCDs done early;
 // now 187).  Samples of few units, which do not divide by eight, are taken together.  False: no unit.
-__host__ __device__ inline long long xattn_part(long long per_sample, int B) { return per_sample >= 64 ? per_sample : per_sample * B; }
-__device__ __forceinline__ bool xattn_unit(long long per_sample, int B, long long& unit) {
-  const long long part = xattn_part(per_sample, B), per = (part + 7) >> 3, slot = blockIdx.x >> 3, which = slot / per;
-  const long long in_part = (blockIdx.x & 7) * per + (slot - which * per);
+// (All counts are below 2^31: divisions of 32 bits.)
+__host__ __device__ inline unsigned xattn_part(unsigned per_sample, unsigned B) { return per_sample >= 64 ? per_sample : per_sample * B; }
+__device__ __forceinline__ bool xattn_unit(unsigned per_sample, unsigned B, unsigned& unit, unsigned number = blockIdx.x) {
+  const unsigned part = xattn_part(per_sample, B), per = (part + 7) >> 3, slot = number >> 3, which = slot / per;
+  const unsigned in_part = (number & 7) * per + (slot - which * per);
   unit = which * part + in_part;
   return in_part < part && unit < per_sample * B;
 }
-static unsigned xattn_grid(long long per_sample, int B) {
-  const long long part = xattn_part(per_sample, B);
-  return (unsigned)(8 * ((part + 7) / 8) * (per_sample * B / part));
+// Numbers of workgroups that have a unit, and some that have none.
+__host__ __device__ inline unsigned xattn_numbers(unsigned per_sample, unsigned B) {
+  const unsigned part = xattn_part(per_sample, B);
+  return 8 * ((part + 7) / 8) * (per_sample * B / part);
 }
+
+// TileCopy for rows that are 16-byte aligned whatever the strides are.
+template <int WAVES>
+struct AlignedCopy : TileCopy<WAVES> {
+  template <bool ZEROS = false>
+  __device__ __forceinline__ void tile(int row0, int N, unsigned lds_tile) const {
+    const unsigned to = this->dst(lds_tile);
+    if (__builtin_expect(this->plain(row0, 32, N), 1)) {
+      const char* b = this->slice + row0 * this->snb;
+#pragma unroll
+      for (int i = 0; i < this->PPW; ++i) copy_piece(i < 4 ? b : b + 16 * this->snb, this->off[i & 3], to + i * 1024);
+      return;
+    }
+    int ln = this->lane;
+    asm volatile("" : "+v"(ln));              // (nothing of this path is worth a register outside of it)
+#pragma unroll 1
+    for (int i = 0; i < this->PPW; ++i) {
+      const int r = 4 * (this->PPW * this->w + i) + (ln >> 4);
+      if (ZEROS && row0 + r >= N)
+        *(__attribute__((address_space(3))) v4i*)(uintptr_t)(to + i * 1024 + ln * 16) = v4i{};
+      else
+        copy_piece(this->slice + min(row0 + r, N - 1) * this->snb + (((ln & 15) ^ swz(r)) << 4), to + i * 1024);
+    }
+  }
+};
 
 __device__ __forceinline__ int xattn_len(const XattnArgs& a, int b) {
   return a.lens ? min(max(__builtin_amdgcn_readfirstlane(a.lens[b]), 0), a.Nk) : a.Nk;
@@ -93,11 +120,11 @@ template <int NW, bool LSE, bool SPLIT>
 __global__ void __launch_bounds__(NW * 64, 2) xattn_fwd_kernel(XattnArgs a) {
   constexpr int KT = NW == 4 ? 2 : 1, STEP_B = 2 * KT * SWZ_TILE_B, STEP = 32 * KT;
   __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];   // two steps' tiles: KT of K, then KT of V
-  long long unit;
-  if (!xattn_unit((long long)a.G * a.fwd.splits * a.fwd.tiles, a.B, unit)) return;
-  const int tile = (int)(unit % a.fwd.tiles), rest = (int)(unit / a.fwd.tiles);
-  const int split = SPLIT ? rest % a.fwd.splits : 0, bg = SPLIT ? rest / a.fwd.splits : rest;
-  const int b = bg / a.G, g = bg - b * a.G;
+  unsigned unit;
+  if (!xattn_unit((unsigned)a.G * a.fwd.splits * a.fwd.tiles, a.B, unit)) return;
+  const int rest = unit / (unsigned)a.fwd.tiles, tile = unit - (unsigned)rest * a.fwd.tiles;
+  const int split = SPLIT ? (unsigned)rest % (unsigned)a.fwd.splits : 0, bg = SPLIT ? (unsigned)rest / (unsigned)a.fwd.splits : rest;
+  const int b = (unsigned)bg / (unsigned)a.G, g = bg - b * a.G;
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
   const int len = xattn_len(a, b), k0 = SPLIT ? split * a.fwd.chunk : 0, k1 = SPLIT ? min(len, k0 + a.fwd.chunk) : len;
   const int r0 = (tile * NW + w) * 32, row = r0 + l32;
@@ -110,7 +137,7 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_fwd_kernel(XattnArgs a) {
   v16f lacc = v16f{};    // register 0: the running sum of the rounded weights
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
   if (k0 < k1) {
-    TileCopy<NW> ck, cv;
+    AlignedCopy<NW> ck, cv;
     ck.init(a.k + b * a.lk.sb + g * a.lk.sh, a.lk.sn, w, lane);
     cv.init(a.v + b * a.lv.sb + g * a.lv.sh, a.lv.sn, w, lane);
     const int n_off = swz_lane_offset(l32, hf), t_off = swz_tr_lane_offset(lane);
@@ -300,11 +327,11 @@ template <int NW, bool SPLIT>
 __global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
   constexpr int KT = NW == 4 ? 2 : 1, STEP_B = 2 * KT * SWZ_TILE_B, STEP = 32 * KT;
   __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];
-  long long unit;
-  if (!xattn_unit((long long)a.G * a.dqd.splits * a.dqd.tiles, a.B, unit)) return;
-  const int tile = (int)(unit % a.dqd.tiles), rest = (int)(unit / a.dqd.tiles);
-  const int split = SPLIT ? rest % a.dqd.splits : 0, bg = SPLIT ? rest / a.dqd.splits : rest;
-  const int b = bg / a.G, g = bg - b * a.G;
+  unsigned unit;
+  if (!xattn_unit((unsigned)a.G * a.dqd.splits * a.dqd.tiles, a.B, unit)) return;
+  const int rest = unit / (unsigned)a.dqd.tiles, tile = unit - (unsigned)rest * a.dqd.tiles;
+  const int split = SPLIT ? (unsigned)rest % (unsigned)a.dqd.splits : 0, bg = SPLIT ? (unsigned)rest / (unsigned)a.dqd.splits : rest;
+  const int b = (unsigned)bg / (unsigned)a.G, g = bg - b * a.G;
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
   const int len = xattn_len(a, b), k0 = SPLIT ? split * a.dqd.chunk : 0, k1 = SPLIT ? min(len, k0 + a.dqd.chunk) : len;
   const int r0 = (tile * NW + w) * 32, row = r0 + l32;
@@ -345,7 +372,7 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
         }
       }
     }
-    TileCopy<NW> ck, cv;
+    AlignedCopy<NW> ck, cv;
     ck.init(a.k + b * a.lk.sb + g * a.lk.sh, a.lk.sn, w, lane);
     cv.init(a.v + b * a.lv.sb + g * a.lv.sh, a.lv.sn, w, lane);
     const int n_off = swz_lane_offset(l32, hf), t_off = swz_tr_lane_offset(lane);
@@ -409,11 +436,11 @@ template <int NW, bool SPLIT>
 __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) xattn_dkv_kernel(XattnArgs a) {
   constexpr int QT = 2, STEP_B = 2 * QT * SWZ_TILE_B + 512, STEP = 32 * QT, DEEP = 2;  // Q, dO, then lse2 and -delta of the rows
   __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];
-  long long unit;
-  if (!xattn_unit((long long)a.G * a.dkv.splits * a.dkv.tiles, a.B, unit)) return;
-  const int tile = (int)(unit % a.dkv.tiles), rest = (int)(unit / a.dkv.tiles);
-  const int split = SPLIT ? rest % a.dkv.splits : 0, bg = SPLIT ? rest / a.dkv.splits : rest;
-  const int b = bg / a.G, g = bg - b * a.G;
+  unsigned unit;
+  if (!xattn_unit((unsigned)a.G * a.dkv.splits * a.dkv.tiles, a.B, unit)) return;
+  const int rest = unit / (unsigned)a.dkv.tiles, tile = unit - (unsigned)rest * a.dkv.tiles;
+  const int split = SPLIT ? (unsigned)rest % (unsigned)a.dkv.splits : 0, bg = SPLIT ? (unsigned)rest / (unsigned)a.dkv.splits : rest;
+  const int b = (unsigned)bg / (unsigned)a.G, g = bg - b * a.G;
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
   const int len = xattn_len(a, b), key0 = (tile * NW + w) * 32, key = key0 + l32;
   const int per_head = (a.Nq + STEP - 1) / STEP, total = a.group * per_head;
@@ -426,13 +453,13 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) xattn_dkv_kernel(Xat
     uint4 kf[8], vf[8];
     own_rows(a.k + b * a.lk.sb + g * a.lk.sh, a.lk.sn, key, len, hf, kf);
     own_rows(a.v + b * a.lv.sb + g * a.lv.sh, a.lv.sn, key, len, hf, vf);
-    TileCopy<NW> cq, cd;
+    AlignedCopy<NW> cq, cd;
     const bf16_t *q0 = a.q + b * a.lq.sb + (long long)g * a.group * a.lq.sh, *d0 = a.dout + b * a.ldo.sb + (long long)g * a.group * a.ldo.sh;
     cq.init(q0, a.lq.sn, w, lane);
     cd.init(d0, a.ldo.sn, w, lane);
     const long long stat0 = ((long long)b * a.H + g * a.group) * xattn_padded_rows(a.Nq);
     const int n_off = swz_lane_offset(l32, hf), t_off = swz_tr_lane_offset(lane);
-    int head = s0 / per_head, in_head = s0 - head * per_head;   // of the step requested next
+    int head = (unsigned)s0 / (unsigned)per_head, in_head = s0 - head * per_head;   // of the step requested next
     auto request = [&](int half) __attribute__((always_inline)) {
       cq.slice = (const char*)(q0 + head * a.lq.sh);
       cd.slice = (const char*)(d0 + head * a.ldo.sh);
@@ -592,7 +619,7 @@ XattnDeal xattn_deal_keys(int B, int G, int group, int Nq, int Nk) {
 }
 
 void launch_xattn_fwd(const XattnArgs& a, hipStream_t stream) {
-  const unsigned grid = xattn_grid((long long)a.G * a.fwd.splits * a.fwd.tiles, a.B);
+  const unsigned grid = xattn_numbers((unsigned)a.G * a.fwd.splits * a.fwd.tiles, a.B);
 #define XATTN_FWD(NW)                                                                                                          \
   do {                                                                                                                         \
     if (a.fwd.splits > 1) {                                                                                                    \
@@ -616,7 +643,7 @@ void launch_xattn_fwd(const XattnArgs& a, hipStream_t stream) {
 
 void launch_xattn_bwd(const XattnArgs& a, hipStream_t stream) {
   const long long all = (long long)a.B * a.H * a.Nq;
-  const unsigned gq = xattn_grid((long long)a.G * a.dqd.splits * a.dqd.tiles, a.B), gk = xattn_grid((long long)a.G * a.dkv.splits * a.dkv.tiles, a.B);
+  const unsigned gq = xattn_numbers((unsigned)a.G * a.dqd.splits * a.dqd.tiles, a.B), gk = xattn_numbers((unsigned)a.G * a.dkv.splits * a.dkv.tiles, a.B);
 #define XATTN_BWD(KERNEL, NW, SPLIT, GRID)                                    \
   do {                                                                        \
     if (SPLIT) KERNEL<NW, true><<<GRID, NW * 64, 0, stream>>>(a);             \
