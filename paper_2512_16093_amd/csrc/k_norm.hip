@@ -7,10 +7,11 @@
 
 namespace sla {
 
-__device__ __forceinline__ uint4 load_row(const bf16_t* row, int e) { return *(const uint4*)(row + 8ll * e); }
+template <bool NT = false>
+__device__ __forceinline__ uint4 load_row(const bf16_t* row, int e) { return load_from<NT, uint4>(row + 8ll * e); }
 
 // STATS: h and r instead of h and y.
-template <int T, int CH, bool STATS>
+template <int T, int CH, bool STATS, bool NT>
 __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_fwd_kernel(const bf16_t* __restrict__ x, const bf16_t* __restrict__ res,
                                                                          const bf16_t* __restrict__ weight, bf16_t* __restrict__ h,
                                                                          bf16_t* __restrict__ y, float* __restrict__ r_out, int M, int K,
@@ -25,8 +26,8 @@ __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_fwd_kernel(const 
     for (int c = 0; c < CH; ++c) {
       v[c] = add[c] = uint4{0u, 0u, 0u, 0u};
       if (t + c * T < n) {
-        v[c] = load_row(x + m * K, t + c * T);
-        if (res) add[c] = load_row(res + m * K, t + c * T);
+        v[c] = load_row<NT>(x + m * K, t + c * T);
+        if (res) add[c] = load_row<NT>(res + m * K, t + c * T);
       }
     }
     float ss = 0.f;
@@ -40,7 +41,7 @@ __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_fwd_kernel(const 
 #pragma unroll
         for (int i = 0; i < 8; ++i) a[i] += b[i];
         v[c] = pack8(a);
-        if (t + c * T < n) *(uint4*)(h + m * K + 8ll * (t + c * T)) = v[c];
+        if (t + c * T < n) store_to<NT>(h + m * K + 8ll * (t + c * T), v[c]);
         unpack8(v[c], a);
       }
 #pragma unroll
@@ -64,14 +65,14 @@ __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_fwd_kernel(const 
 #pragma unroll
           for (int i = 0; i < 8; ++i) a[i] *= r;
         }
-        *(uint4*)(y + m * K + 8ll * (t + c * T)) = pack8(a);
+        store_to<NT>(y + m * K + 8ll * (t + c * T), pack8(a));
       }
     }
   }
 }
 
 // dx, and each workgroup's share of dw in registers over the rows it takes.
-template <int T, int CH>
+template <int T, int CH, bool NT>
 __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_bwd_kernel(const bf16_t* __restrict__ dy, const bf16_t* __restrict__ dh,
                                                                          const bf16_t* __restrict__ h, const bf16_t* __restrict__ weight,
                                                                          bf16_t* __restrict__ dx, float* __restrict__ part, int M, int K,
@@ -89,9 +90,9 @@ __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_bwd_kernel(const 
     for (int c = 0; c < CH; ++c) {
       rg[c] = rx[c] = rh[c] = uint4{0u, 0u, 0u, 0u};
       if (t + c * T < n) {
-        rg[c] = load_row(dy + m * K, t + c * T);
-        rx[c] = load_row(h + m * K, t + c * T);
-        if (dh) rh[c] = load_row(dh + m * K, t + c * T);
+        rg[c] = load_row<NT>(dy + m * K, t + c * T);
+        rx[c] = load_row<NT>(h + m * K, t + c * T);
+        if (dh) rh[c] = load_row<NT>(dh + m * K, t + c * T);
       }
     }
     // of one share: h, w dy, and dy h (the share of dw is r times that)
@@ -138,7 +139,7 @@ __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_bwd_kernel(const 
         dw[c][i] = __builtin_fmaf(gx[i], r, dw[c][i]);
         up[i] += __builtin_fmaf(g[i], r, -x[i] * dot);
       }
-      if (t + c * T < n) *(uint4*)(dx + m * K + 8ll * (t + c * T)) = pack8(up);
+      if (t + c * T < n) store_to<NT>(dx + m * K + 8ll * (t + c * T), pack8(up));
     }
   }
   if (!part) return;
@@ -194,18 +195,25 @@ __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_bwd_kernel(const 
     else F(1024, 2);                      \
   } while (0)
 
+// `tensors` of these that do not fit the memory-side cache together are read and written past it.
+static bool streams(int M, int K, int tensors) { return (long long)M * K * 2 * tensors > (256ll << 20); }
 static unsigned row_workgroups(int M, int T) { return (unsigned)min(T == 64 ? (M + 3) / 4 : M, 1 << 20); }
 
 void launch_norm_fwd(const void* x, const void* res, const void* w, void* h, void* y, int M, int K, float eps, hipStream_t stream) {
 #define NORM_FWD(T, CH)                                                                                                   \
-  norm_fwd_kernel<T, CH, false><<<row_workgroups(M, T), T == 1024 ? 1024 : 256, 0, stream>>>(                             \
+  do {                                                                                                                    \
+    if (streams(M, K, res ? 4 : 2)) NORM_FWD_(T, CH, true); else NORM_FWD_(T, CH, false);                                 \
+  } while (0)
+#define NORM_FWD_(T, CH, NT)                                                                                              \
+  norm_fwd_kernel<T, CH, false, NT><<<row_workgroups(M, T), T == 1024 ? 1024 : 256, 0, stream>>>(                         \
       (const bf16_t*)x, (const bf16_t*)res, (const bf16_t*)w, (bf16_t*)h, (bf16_t*)y, nullptr, M, K, eps)
   NORM_TEAMS(K, NORM_FWD);
+#undef NORM_FWD_
 #undef NORM_FWD
 }
 void launch_norm_stats(const void* x, const void* res, void* h, float* r, int M, int K, float eps, hipStream_t stream) {
 #define NORM_STATS(T, CH)                                                                                                 \
-  norm_fwd_kernel<T, CH, true><<<row_workgroups(M, T), T == 1024 ? 1024 : 256, 0, stream>>>(                              \
+  norm_fwd_kernel<T, CH, true, false><<<row_workgroups(M, T), T == 1024 ? 1024 : 256, 0, stream>>>(                              \
       (const bf16_t*)x, (const bf16_t*)res, nullptr, (bf16_t*)h, nullptr, r, M, K, eps)
   NORM_TEAMS(K, NORM_STATS);
 #undef NORM_STATS
@@ -220,9 +228,14 @@ void launch_norm_bwd(const void* dy, const void* dh, const void* h, const void* 
   if (!dw) part = nullptr;
   const unsigned grid = (unsigned)norm_bwd_workgroups(M, K);
 #define NORM_BWD(T, CH)                                                                                                   \
-  norm_bwd_kernel<T, CH><<<grid, T == 1024 ? 1024 : 256, 0, stream>>>((const bf16_t*)dy, (const bf16_t*)dh, (const bf16_t*)h, \
-                                                                     (const bf16_t*)w, (bf16_t*)dx, part, M, K, eps)
+  do {                                                                                                                    \
+    if (streams(M, K, dh ? 4 : 3)) NORM_BWD_(T, CH, true); else NORM_BWD_(T, CH, false);                                  \
+  } while (0)
+#define NORM_BWD_(T, CH, NT)                                                                                              \
+  norm_bwd_kernel<T, CH, NT><<<grid, T == 1024 ? 1024 : 256, 0, stream>>>((const bf16_t*)dy, (const bf16_t*)dh, (const bf16_t*)h, \
+                                                                         (const bf16_t*)w, (bf16_t*)dx, part, M, K, eps)
   NORM_TEAMS(K, NORM_BWD);
+#undef NORM_BWD_
 #undef NORM_BWD
   PartialSums s{};
   s.part[0] = part;

@@ -46,19 +46,19 @@ __device__ __forceinline__ void token_angles(const RopeArgs& a, long long b, lon
 }
 
 // Four pairs of a head: the words of part `part` of its 256 bytes, and their numbers lo[i], hi[i].
-template <bool HALVES>
+template <bool HALVES, bool NT>
 __device__ __forceinline__ uint4 load_pairs(const bf16_t* head, int part) {
-  if constexpr (!HALVES) return *(const uint4*)(head + 8 * part);
-  const uint2 lo = *(const uint2*)(head + 4 * part), hi = *(const uint2*)(head + D / 2 + 4 * part);
+  if constexpr (!HALVES) return load_from<NT, uint4>(head + 8 * part);
+  const uint2 lo = load_from<NT, uint2>(head + 4 * part), hi = load_from<NT, uint2>(head + D / 2 + 4 * part);
   return uint4{lo.x, lo.y, hi.x, hi.y};
 }
-template <bool HALVES>
+template <bool HALVES, bool NT>
 __device__ __forceinline__ void store_pairs(bf16_t* head, int part, const uint4& v) {
   if constexpr (!HALVES) {
-    *(uint4*)(head + 8 * part) = v;
+    store_to<NT>(head + 8 * part, v);
   } else {
-    *(uint2*)(head + 4 * part) = uint2{v.x, v.y};
-    *(uint2*)(head + D / 2 + 4 * part) = uint2{v.z, v.w};
+    store_to<NT>(head + 4 * part, uint2{v.x, v.y});
+    store_to<NT>(head + D / 2 + 4 * part, uint2{v.z, v.w});
   }
 }
 template <bool HALVES>
@@ -85,7 +85,7 @@ __device__ __forceinline__ uint4 pack_pairs(const float (&lo)[4], const float (&
 template <int NORM, bool HALVES>
 __device__ __forceinline__ void weight_pairs(const bf16_t* w, int head, int part, float (&lo)[4], float (&hi)[4]) {
   if (w) {
-    unpack_pairs<HALVES>(load_pairs<HALVES>(w + (NORM == 2 ? head * D : 0), part), lo, hi);
+    unpack_pairs<HALVES>(load_pairs<HALVES, false>(w + (NORM == 2 ? head * D : 0), part), lo, hi);
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) lo[i] = hi[i] = 1.0f;
@@ -99,7 +99,7 @@ __device__ __forceinline__ float pair_dot(const float (&al)[4], const float (&ah
 }
 
 // NORM: rope_norm.  T: threads of a team (64: up to 16 heads, 256: up to 64); CH: a thread's shares of a token.
-template <int T, int CH, int NORM, bool HALVES>
+template <int T, int CH, int NORM, bool HALVES, bool NT>
 __global__ void __launch_bounds__(256) rope_fwd_kernel(RopeArgs a) {
   __shared__ float2 angles[4][64];
   __shared__ float red[2][4];
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(256) rope_fwd_kernel(RopeArgs a) {
     for (int c = 0; c < CH; ++c) {
       const int head = e0 + c * (T / 16);
       raw[i][c] = uint4{0u, 0u, 0u, 0u};
-      if (head < x.H) raw[i][c] = load_pairs<HALVES>(x.x + b * x.lx.sb + head * x.lx.sh + n * x.lx.sn, part);
+      if (head < x.H) raw[i][c] = load_pairs<HALVES, NT>(x.x + b * x.lx.sb + head * x.lx.sh + n * x.lx.sn, part);
     }
   }
   float2 cs[4];
@@ -157,13 +157,13 @@ __global__ void __launch_bounds__(256) rope_fwd_kernel(RopeArgs a) {
         yl[j] = __builtin_fmaf(lo[j], cs[j].x, -hi[j] * cs[j].y);
         yh[j] = __builtin_fmaf(lo[j], cs[j].y, hi[j] * cs[j].x);
       }
-      store_pairs<HALVES>(x.y + b * x.ly.sb + head * x.ly.sh + n * x.ly.sn, part, pack_pairs<HALVES>(yl, yh));
+      store_pairs<HALVES, NT>(x.y + b * x.ly.sb + head * x.ly.sh + n * x.ly.sn, part, pack_pairs<HALVES>(yl, yh));
     }
   }
 }
 
 // Gradients, blockIdx.y: q or k.  Each team takes every (teams)-th token.
-template <int T, int CH, int NORM, bool HALVES>
+template <int T, int CH, int NORM, bool HALVES, bool NT>
 __global__ void __launch_bounds__(256) rope_bwd_kernel(RopeArgs a) {
   __shared__ float2 angles[4][64];
   __shared__ float red[2][4];
@@ -183,8 +183,8 @@ __global__ void __launch_bounds__(256) rope_bwd_kernel(RopeArgs a) {
       const int head = e0 + c * (T / 16);
       rg[c] = rx[c] = uint4{0u, 0u, 0u, 0u};
       if (head < x.H) {
-        rg[c] = load_pairs<HALVES>(x.dy + b * x.ldy.sb + head * x.ldy.sh + n * x.ldy.sn, part);
-        if constexpr (NORM != 0) rx[c] = load_pairs<HALVES>(x.x + b * x.lx.sb + head * x.lx.sh + n * x.lx.sn, part);
+        rg[c] = load_pairs<HALVES, NT>(x.dy + b * x.ldy.sb + head * x.ldy.sh + n * x.ldy.sn, part);
+        if constexpr (NORM != 0) rx[c] = load_pairs<HALVES, NT>(x.x + b * x.lx.sb + head * x.lx.sh + n * x.lx.sn, part);
       }
     }
     float2 cs[4];
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(256) rope_bwd_kernel(RopeArgs a) {
       }
     };
     auto put = [&](int head, const float (&gl)[4], const float (&gh)[4]) __attribute__((always_inline)) {
-      store_pairs<HALVES>(x.y + b * x.ly.sb + head * x.ly.sh + n * x.ly.sn, part, pack_pairs<HALVES>(gl, gh));
+      store_pairs<HALVES, NT>(x.y + b * x.ly.sb + head * x.ly.sh + n * x.ly.sn, part, pack_pairs<HALVES>(gl, gh));
     };
     float r = 1.0f, dot = 0.f;
     if constexpr (NORM == 2) {
@@ -357,20 +357,30 @@ void launch_sum_partials(const PartialSums& s, hipStream_t stream) {
 }
 
 // ---------------------------------------------------------------------------
-template <int T, int CH, int NORM, bool HALVES>
+// The call's tensors do not fit the memory-side cache: they are read and written past it (75600 x 40 heads, token-major, forward
+// 568 -> 516 us without a norm, 543 -> 536 with one over the token; 32760 x 12 78 -> 66); where they fit, that costs (4096 x 24 heads,
+// the norm over the token 20 -> 23 us).
+static bool streams(const RopeArgs& a, bool bwd) {
+  const long long elems = (long long)a.B * a.N * (a.t[0].H + a.t[1].H) * D;
+  return elems * 2 * (bwd && a.t[0].x ? 3 : 2) > (256ll << 20);
+}
+template <int T, int CH, int NORM, bool HALVES, bool NT>
 static void launch_rope(const RopeArgs& a, bool bwd, hipStream_t stream) {
   const long long tokens = (long long)a.B * a.N;
   if (bwd) {
     const int heads = max(a.t[0].H, a.t[1].H);
-    rope_bwd_kernel<T, CH, NORM, HALVES><<<dim3((unsigned)rope_bwd_workgroups(tokens, heads), a.t[1].H ? 2 : 1), 256, 0, stream>>>(a);
+    rope_bwd_kernel<T, CH, NORM, HALVES, NT><<<dim3((unsigned)rope_bwd_workgroups(tokens, heads), a.t[1].H ? 2 : 1), 256, 0, stream>>>(a);
   } else {
-    rope_fwd_kernel<T, CH, NORM, HALVES><<<(unsigned)(T == 64 ? (tokens + 3) / 4 : tokens), 256, 0, stream>>>(a);
+    rope_fwd_kernel<T, CH, NORM, HALVES, NT><<<(unsigned)(T == 64 ? (tokens + 3) / 4 : tokens), 256, 0, stream>>>(a);
   }
 }
 template <int T, int CH, int NORM>
 static void launch_rope(const RopeArgs& a, bool bwd, bool halves, hipStream_t stream) {
-  if (halves) launch_rope<T, CH, NORM, true>(a, bwd, stream);
-  else launch_rope<T, CH, NORM, false>(a, bwd, stream);
+  const bool nt = streams(a, bwd);
+  if (halves && nt) launch_rope<T, CH, NORM, true, true>(a, bwd, stream);
+  else if (halves) launch_rope<T, CH, NORM, true, false>(a, bwd, stream);
+  else if (nt) launch_rope<T, CH, NORM, false, true>(a, bwd, stream);
+  else launch_rope<T, CH, NORM, false, false>(a, bwd, stream);
 }
 template <int T, int CH>
 static void launch_rope(const RopeArgs& a, bool bwd, int norm, bool halves, hipStream_t stream) {

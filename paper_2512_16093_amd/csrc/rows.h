@@ -47,6 +47,19 @@ struct PartialSums {
 };
 void launch_sum_partials(const PartialSums& s, hipStream_t stream);
 
+// Sixteen (eight) bytes from and to memory; NT: past the caches.
+template <bool NT, class V>
+__device__ __forceinline__ V load_from(const bf16_t* p) {
+  typedef int words __attribute__((ext_vector_type(sizeof(V) / 4)));
+  if constexpr (NT) return __builtin_bit_cast(V, __builtin_nontemporal_load((const words*)p));
+  else return *(const V*)p;
+}
+template <bool NT, class V>
+__device__ __forceinline__ void store_to(bf16_t* p, const V& v) {
+  typedef int words __attribute__((ext_vector_type(sizeof(V) / 4)));
+  if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(words, v), (words*)p);
+  else *(V*)p = v;
+}
 // A team of T threads (64: a wavefront, four teams to a workgroup; else the workgroup).  sum(): of one number per thread,
 // to all of them; red: T / 64 floats of shared memory that the sum before the last one may still be read from (callers
 // alternate between two).
