@@ -219,9 +219,12 @@ void launch_norm_stats(const void* x, const void* res, void* h, float* r, int M,
 #undef NORM_STATS
 }
 
+// Each workgroup leaves a row of partial sums of dw: at least eight rows (of each team) for one of those, but enough workgroups to
+// fill the chip.  In us, with 256 / 512 / 1024 workgroups: 2048 x 5120 28.2 / 26.2 / 29.0, 4096 x 5120 45.5 / 38.9 / 39.6, 8192 x 5120
+// 96.2 / 79.3 / 75.2, 8192 x 1536 29.3 / 26.4 / 27.8; of 1024 threads, 2048 x 13824 46.3 / 53.1 / 68.8, 8192 x 13824 with 512 181.
 int norm_bwd_workgroups(int M, int K) {
-  const int all = K <= 2048 ? (M + 3) / 4 : M;
-  return min(all, K <= 8192 ? 1024 : 512);
+  const int all = K <= 2048 ? (M + 3) / 4 : M, least = K <= 8192 ? 512 : 256;
+  return min(all, max(least, min(all / 8, 2 * least)));
 }
 void launch_norm_bwd(const void* dy, const void* dh, const void* h, const void* w, void* dx, float* dw, float* part, int M, int K,
                      float eps, hipStream_t stream) {

@@ -35,8 +35,8 @@ __device__ __forceinline__ float2 cos_sin(uint64_t t) {
 }
 
 // A token's angles to a wavefront's 64 entries of LDS, then the four of this lane's pairs (4 part .. 4 part + 3).
-__device__ __forceinline__ void token_angles(const RopeArgs& a, long long b, long long n, float2* mine, int lane, float2 (&cs)[4]) {
-  const int32_t p = a.pos[b * a.pos_batch + 3 * n + a.plan.axis[lane]];
+__device__ __forceinline__ void token_angles(const RopeArgs& a, int b, int n, float2* mine, int lane, float2 (&cs)[4]) {
+  const int32_t p = a.pos[b * a.pos_batch + 3ll * n + a.plan.axis[lane]];
   __builtin_amdgcn_wave_barrier();      // (a wavefront's LDS operations execute in order: only the compiler has to keep it)
   mine[lane] = cos_sin((uint64_t)(int64_t)p * a.plan.turns[lane]);
   __builtin_amdgcn_wave_barrier();
@@ -104,9 +104,9 @@ __global__ void __launch_bounds__(256) rope_fwd_kernel(RopeArgs a) {
   __shared__ float2 angles[4][64];
   __shared__ float red[2][4];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, part = lane & 15, e0 = (T == 64 ? lane : t) >> 4;
-  const long long tok = T == 64 ? 4ll * blockIdx.x + w : blockIdx.x;
-  if (T == 64 && tok >= (long long)a.B * a.N) return;
-  const long long b = tok / a.N, n = tok - b * a.N;
+  const int tok = T == 64 ? 4 * blockIdx.x + w : blockIdx.x;                 // (below 2^24)
+  if (T == 64 && tok >= a.B * a.N) return;
+  const int b = tok / a.N, n = tok - b * a.N;
   uint4 raw[2][CH];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -171,12 +171,12 @@ __global__ void __launch_bounds__(256) rope_bwd_kernel(RopeArgs a) {
   __shared__ float4 join[NORM == 0 ? 1 : ACC * 2 * 64];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, part = lane & 15, e0 = (T == 64 ? lane : t) >> 4;
   const RopeTensor& x = a.t[blockIdx.y];
-  const long long tokens = (long long)a.B * a.N;
+  const int tokens = a.B * a.N;                // (below 2^24)
   const float inv = NORM == 2 ? 1.0f / (float)(x.H * D) : 1.0f / D;
   float dwl[ACC][4] = {}, dwh[ACC][4] = {};
   int turn = 0;
-  for (long long tok = T == 64 ? 4ll * blockIdx.x + w : blockIdx.x; tok < tokens; tok += (long long)gridDim.x * (256 / T), turn ^= 1) {
-    const long long b = tok / a.N, n = tok - b * a.N;
+  for (int tok = T == 64 ? 4 * blockIdx.x + w : blockIdx.x; tok < tokens; tok += gridDim.x * (256 / T), turn ^= 1) {
+    const int b = tok / a.N, n = tok - b * a.N;
     uint4 rg[CH], rx[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -368,8 +368,9 @@ template <int T, int CH, int NORM, bool HALVES, bool NT>
 static void launch_rope(const RopeArgs& a, bool bwd, hipStream_t stream) {
   const long long tokens = (long long)a.B * a.N;
   if (bwd) {
-    const int heads = max(a.t[0].H, a.t[1].H);
-    rope_bwd_kernel<T, CH, NORM, HALVES, NT><<<dim3((unsigned)rope_bwd_workgroups(tokens, heads), a.t[1].H ? 2 : 1), 256, 0, stream>>>(a);
+    // (without a weight to sum up for there is nothing to walk for: 75600 x 40 heads 643 us with 512 workgroups, 617 with 2048)
+    const int heads = max(a.t[0].H, a.t[1].H), groups = NORM == 0 ? (int)min((tokens * T + 255) / 256, 1ll << 16) : rope_bwd_workgroups(tokens, heads);
+    rope_bwd_kernel<T, CH, NORM, HALVES, NT><<<dim3((unsigned)groups, a.t[1].H ? 2 : 1), 256, 0, stream>>>(a);
   } else {
     rope_fwd_kernel<T, CH, NORM, HALVES, NT><<<(unsigned)(T == 64 ? (tokens + 3) / 4 : tokens), 256, 0, stream>>>(a);
   }
@@ -400,6 +401,9 @@ static void launch_rope(const RopeArgs& a, bool bwd, int norm, bool halves, hipS
   else launch_rope<256, 4>(a, bwd, norm, halves, stream);
 }
 
+// Two to a compute unit and tensor: what it holds (8192 tokens of 24 heads, in us: 128 workgroups 145, 256 90, 512 78; 75600 of 40 heads
+// 512 962, 1024 957, 32760 of 12 121 and 125).  The next token's rows requested ahead cost more in wavefronts than they hid
+// (75600 of 40 heads 1067 us).
 int rope_bwd_workgroups(long long tokens, int heads) {
   const long long all = heads <= 16 ? (tokens + 3) / 4 : tokens;
   return (int)min(all, 512ll);

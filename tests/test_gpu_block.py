@@ -80,7 +80,7 @@ def test_inference_chain(grid, prompt):
     for i, (name, w) in enumerate((("q", blk.qn), ("k", blk.kn))):
         assert _rel(e[name], bo.rope_fwd(qkv[i], ang, "interleaved", _np(w), "token")) < 2 ** -9
     v = e["qkv"].view(1, blk.N, 3, H, D)[:, :, 2].permute(0, 2, 1, 3)
-    same = sla.sla_attention_fwd(e["q"], e["k"], v.contiguous(), 64, 64, 0.3, 0.3)
+    same = sla.sla_attention_fwd(e["q"].contiguous(), e["k"].contiguous(), v.contiguous(), 64, 64, 0.3, 0.3)
     assert torch.equal(same, blk.heads(e["att"]))
     assert torch.equal(e["h1"].cpu(), (x.float() + e["att_out"].float()).bfloat16().cpu())
     assert _rel(e["cq"], plain(e64["h1"], blk.n2, blk.w_q, K)) < 1e-2
