@@ -6,13 +6,12 @@
 
 #include "common.h"
 #include "host.h"
-#include "rows.h"
 
 namespace sla {
 void launch_w8a8_quantize(const void* a, int R, int K, int RP, bool negate_odd, int8_t* codes, float* scales,
                           hipStream_t stream);
-void launch_w8a8_quantize_normed(const void* a, const float* r, const void* w, int R, int K, int RP, int8_t* codes, float* scales,
-                                 hipStream_t stream);
+void launch_w8a8_quantize_normed(const void* x, const void* res, const void* w, void* h, float* r, float eps, int R, int K, int RP,
+                                 int8_t* codes, float* scales, hipStream_t stream);
 void launch_w8a8_unpack(const int8_t* frag, const float* s, int R, int K, int RP, bool negate_odd, int8_t* codes,
                         float* scales, hipStream_t stream);
 void launch_w8a8_gemm(const int8_t* x8, const float* sx, int MP, const int8_t* w8, const float* sw,
@@ -100,8 +99,7 @@ int w8a8_norm_quantize_act(const void* x, const void* res, const void* norm_w, v
   int8_t* codes = (int8_t*)workspace;
   float* scales = (float*)((unsigned char*)workspace + codes_bytes(MP, K));
   float* r = (float*)((unsigned char*)workspace + object_bytes(MP, K));
-  launch_norm_stats(x, res, h, r, M, K, (float)eps, (hipStream_t)stream);
-  launch_w8a8_quantize_normed(res ? h : x, r, norm_w, M, K, MP, codes, scales, (hipStream_t)stream);
+  launch_w8a8_quantize_normed(x, res, norm_w, h, r, (float)eps, M, K, MP, codes, scales, (hipStream_t)stream);
   return launch_status();
 }
 

@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_fwd_kernel(const 
 #pragma unroll
         for (int i = 0; i < 8; ++i) a[i] += b[i];
         v[c] = pack8(a);
-        if (t + c * T < n) store_to<NT>(h + m * K + 8ll * (t + c * T), v[c]);
+        if (t + c * T < n) store_to<NT && !STATS>(h + m * K + 8ll * (t + c * T), v[c]);   // (STATS: h is read again at once)
         unpack8(v[c], a);
       }
 #pragma unroll
@@ -213,9 +213,14 @@ void launch_norm_fwd(const void* x, const void* res, const void* w, void* h, voi
 }
 void launch_norm_stats(const void* x, const void* res, void* h, float* r, int M, int K, float eps, hipStream_t stream) {
 #define NORM_STATS(T, CH)                                                                                                 \
-  norm_fwd_kernel<T, CH, true, false><<<row_workgroups(M, T), T == 1024 ? 1024 : 256, 0, stream>>>(                              \
+  do {                                                                                                                    \
+    if (res && streams(M, K, 3)) NORM_STATS_(T, CH, true); else NORM_STATS_(T, CH, false);                                \
+  } while (0)
+#define NORM_STATS_(T, CH, NT)                                                                                            \
+  norm_fwd_kernel<T, CH, true, NT><<<row_workgroups(M, T), T == 1024 ? 1024 : 256, 0, stream>>>(                          \
       (const bf16_t*)x, (const bf16_t*)res, nullptr, (bf16_t*)h, nullptr, r, M, K, eps)
   NORM_TEAMS(K, NORM_STATS);
+#undef NORM_STATS_
 #undef NORM_STATS
 }
 

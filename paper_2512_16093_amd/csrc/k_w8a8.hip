@@ -22,6 +22,7 @@
 //   w8a8_gemm_splitk_kernel  small workgroup tiles whose wavefronts split the contraction, for calls that do not
 //                          give every compute unit a 256 x 128 tile.
 #include "common.h"
+#include "rows.h"
 
 namespace sla {
 
@@ -51,37 +52,40 @@ __host__ __device__ inline size_t w8_chunk(int kb, int RT, int rt, int ks) {
 // negate_odd (weights): the codes of odd feature blocks are stored negated (see W8_BIAS_I).
 // STREAM: the input is read past the caches (it exceeds what the memory-side cache keeps beside the codes, which the
 // product reads next).
-// NORM: what is quantised is x r w, r one factor per row, w (or nothing) one per column: the root-mean-square norm in
-// front of the layer.  It stays in fp32 until its codes, and is never written anywhere.
-template <bool STREAM, bool NORM>
+// NORM (1, 2): what is quantised is x r w, r one factor per row, w (or nothing) one per column: the root-mean-square norm in
+// front of the layer.  It stays in fp32 until its codes, and is never written anywhere.  1: r has been formed (k_norm.hip), and
+// x lately written, its last rows last: the blocks are taken from there, those rows come out of the memory-side cache, and the
+// product, which starts from the first rows, finds their codes there.  2: few rows: each workgroup forms the
+// rows' r by itself (it reads them whole), adds the residual to its own columns and leaves h there.
+constexpr int W8_FEW_ROWS = 4;
+struct NormIn {
+  const float* r;              // 1
+  const bf16_t *w, *res;       // res: 2, or nullptr
+  bf16_t* h;
+  float eps;
+};
+template <bool STREAM, int NORM>
 __global__ void __launch_bounds__(256) w8a8_quantize_kernel(const bf16_t* __restrict__ a, int R, int K, int RP,
                                                             int negate_odd, int8_t* __restrict__ codes,
-                                                            float* __restrict__ scales, const float* __restrict__ row_factor,
-                                                            const bf16_t* __restrict__ col_factor) {
+                                                            float* __restrict__ scales, NormIn norm) {
   __shared__ uint4 blk[QB * QB / 16];
   __shared__ float wave_amax[4];
   const int KB = K / QB, RB = RP / QB, RT = RP / 32;
-  const int rb = blockIdx.x / KB, kb = blockIdx.x % KB;
+  const int rb = NORM == 1 ? RB - 1 - blockIdx.x / KB : blockIdx.x / KB, kb = blockIdx.x % KB;
   const int t = threadIdx.x, cg = t & 15, r0 = t >> 4, lane = t & 63, w = t >> 6;
   uint4 x[8];
   float amax = 0.f;
   float rf[8], cf[8];
-  if constexpr (NORM) {
-    if (col_factor) {
-      unpack8(*(const uint4*)(col_factor + kb * QB + cg * 8), cf);
-    } else {
+  __shared__ float few[NORM == 2 ? W8_FEW_ROWS : 1];
+  auto sum8 = [](const uint4& a, const uint4& b) __attribute__((always_inline)) {   // the stream as it is stored
+    float u[8], v[8];
+    unpack8(a, u);
+    unpack8(b, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) cf[e] = 1.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) rf[i] = rb * QB + r0 + 16 * i < R ? row_factor[rb * QB + r0 + 16 * i] : 0.f;
-  }
-  // column e of this thread's share of row i, given that share's words
-  auto value = [&](int i, const uint32_t (&wd)[4], int e) __attribute__((always_inline)) {
-    const float v = (e & 1) ? bf16_hi(wd[e >> 1]) : bf16_lo(wd[e >> 1]);
-    if constexpr (NORM) return v * rf[i] * cf[e];
-    else return v;
+    for (int e = 0; e < 8; ++e) u[e] += v[e];
+    return pack8(u);
   };
+  // this thread's share of the block
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int row = rb * QB + r0 + 16 * i;
@@ -89,7 +93,54 @@ __global__ void __launch_bounds__(256) w8a8_quantize_kernel(const bf16_t* __rest
     if (row < R) {
       const v4i* src = (const v4i*)(a + (size_t)row * K + kb * QB + cg * 8);
       x[i] = __builtin_bit_cast(uint4, STREAM ? __builtin_nontemporal_load(src) : *src);
+      if constexpr (NORM == 2) {
+        if (norm.res) {
+          x[i] = sum8(x[i], *(const uint4*)(norm.res + (size_t)row * K + kb * QB + cg * 8));
+          *(uint4*)(norm.h + (size_t)row * K + kb * QB + cg * 8) = x[i];
+        }
+      }
     }
+  }
+  if constexpr (NORM == 2) {                   // (rows past the end: no workgroup of their blocks has any to read)
+    for (int row = w; row < min(R - rb * QB, W8_FEW_ROWS); row += 4) {
+      const size_t at = (size_t)(rb * QB + row) * K;
+      float ss = 0.f;
+#pragma unroll 8
+      for (int c = lane; c < K / 8; c += 64) {
+        uint4 v = *(const uint4*)(a + at + 8 * c);
+        if (norm.res) v = sum8(v, *(const uint4*)(norm.res + at + 8 * c));
+        float f[8];
+        unpack8(v, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(f[e], f[e], ss);
+      }
+      ss = rows_sum(row_sum(ss));
+      if (lane == 0) few[row] = __builtin_amdgcn_rsqf(ss / (float)K + norm.eps);
+    }
+    __syncthreads();
+  }
+  if constexpr (NORM != 0) {
+    if (norm.w) {
+      unpack8(*(const uint4*)(norm.w + kb * QB + cg * 8), cf);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) cf[e] = 1.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = rb * QB + r0 + 16 * i;
+      if constexpr (NORM == 1) rf[i] = row < R ? norm.r[row] : 0.f;
+      else rf[i] = row < R ? few[min(r0 + 16 * i, W8_FEW_ROWS - 1)] : 0.f;
+    }
+  }
+  // column e of this thread's share of row i, given that share's words
+  auto value = [&](int i, const uint32_t (&wd)[4], int e) __attribute__((always_inline)) {
+    const float v = (e & 1) ? bf16_hi(wd[e >> 1]) : bf16_lo(wd[e >> 1]);
+    if constexpr (NORM != 0) return v * rf[i] * cf[e];
+    else return v;
+  };
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
     const uint32_t wd[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) amax = fmaxf(amax, fmaxf(fabsf(value(i, wd, 2 * e)), fabsf(value(i, wd, 2 * e + 1))));
@@ -677,16 +728,27 @@ void launch_w8a8_quantize(const void* a, int R, int K, int RP, bool negate_odd, 
   // Above 128 MiB of input the layer gains 1 to 2 % by reading past the caches (75600 x 5120 2.177 -> 2.147 ms,
   // 32760 x 8960 608 -> 591 us); below it loses as much (4096 x 5120 145.6 -> 148.3 us).
   const bool stream_in = (size_t)R * K * 2 > ((size_t)128 << 20);
-#define SLA_QUANTIZE(STREAM) w8a8_quantize_kernel<STREAM, false><<<grid, 256, 0, stream>>>((const bf16_t*)a, R, K, RP, negate_odd ? 1 : 0, codes, scales, nullptr, nullptr)
+#define SLA_QUANTIZE(STREAM) w8a8_quantize_kernel<STREAM, 0><<<grid, 256, 0, stream>>>((const bf16_t*)a, R, K, RP, negate_odd ? 1 : 0, codes, scales, NormIn{})
   if (stream_in) SLA_QUANTIZE(true); else SLA_QUANTIZE(false);
 #undef SLA_QUANTIZE
 }
 
-// The same of x r w (r fp32 [R], w bf16 [K] or nullptr).
-void launch_w8a8_quantize_normed(const void* a, const float* r, const void* w, int R, int K, int RP, int8_t* codes, float* scales,
-                                 hipStream_t stream) {
-  w8a8_quantize_kernel<false, true><<<(unsigned)((RP / QB) * (K / QB)), 256, 0, stream>>>((const bf16_t*)a, R, K, RP, 0, codes, scales,
-                                                                                        r, (const bf16_t*)w);
+// The same of the norm of h = x + res (res nullptr: of x; w nullptr: ones), h written where there is a res; r: fp32 [R], scratch.
+void launch_w8a8_quantize_normed(const void* x, const void* res, const void* w, void* h, float* r, float eps, int R, int K, int RP,
+                                 int8_t* codes, float* scales, hipStream_t stream) {
+  const unsigned grid = (unsigned)((RP / QB) * (K / QB));
+  NormIn norm{r, (const bf16_t*)w, (const bf16_t*)res, (bf16_t*)h, eps};
+  // A launch of its own for the rows' factors takes longer than reading very few rows once per workgroup (in a captured graph, us:
+  // 1 x 5120 6.7 against 7.4, 4 x 5120 6.9, 8 x 5120 9.2, 1 x 1536 5.3; 1 x 13824 9.9 against 8.7).
+  if (R <= W8_FEW_ROWS && K <= 8192) {
+    w8a8_quantize_kernel<false, 2><<<grid, 256, 0, stream>>>((const bf16_t*)x, R, K, RP, 0, codes, scales, norm);
+    return;
+  }
+  launch_norm_stats(x, res, h, r, R, K, eps, stream);
+  // An h beyond the memory-side cache is read past it (its last rows are found there all the same): with the statistics, 75600 x 5120
+  // 640 -> 613 us, 32760 x 5120 271 -> 248; without a residual x is not lately written, and that costs (75600 x 1536 93 -> 103).
+  if (res && (long long)R * K * 2 > (256ll << 20)) w8a8_quantize_kernel<true, 1><<<grid, 256, 0, stream>>>((const bf16_t*)h, R, K, RP, 0, codes, scales, norm);
+  else w8a8_quantize_kernel<false, 1><<<grid, 256, 0, stream>>>((const bf16_t*)(res ? h : x), R, K, RP, 0, codes, scales, norm);
 }
 
 void launch_w8a8_unpack(const int8_t* frag, const float* s, int R, int K, int RP, bool negate_odd, int8_t* codes,
