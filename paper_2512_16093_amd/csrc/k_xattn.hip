@@ -15,6 +15,7 @@
 // workspace.
 #include <algorithm>
 #include <cfloat>
+#include <cmath>
 
 #include "tiles.h"
 #include "xattn.h"
@@ -601,21 +602,30 @@ __global__ void __launch_bounds__(256) xattn_sum_kernel(XattnSum x) {
 }
 
 // ---------------------------------------------------------------------------
-static XattnDeal deal(long long units, int nw, int tiles, int walk, int step, int least, long long places) {
-  // As many pieces as there are places for, none shorter than `least`.
-  const long long most = std::max<long long>(1, walk / least), want = std::max<long long>(1, places / std::max<long long>(1, units));
-  const int pieces = (int)std::min(std::min(most, want), (long long)XATTN_PIECES);
-  int chunk = (walk + pieces - 1) / pieces;
-  chunk = (chunk + step - 1) / step * step;
-  return XattnDeal{nw, tiles, (walk + chunk - 1) / chunk, chunk};
+// A walk of `steps` steps by each of `units` workgroups, of which the chip holds `places` at a time: in how many pieces.  A piece
+// shortens the walk and adds its partial results to what is written and read back (bytes_per_piece at 5 TB/s), and splitting at all
+// adds the launch that joins them.  So the time is  us_per_step * steps / S + 4 us + S * bytes_per_piece / 5 TB/s,  least at
+// S = sqrt(steps us_per_step / (us of a piece)); one piece if that is no more.  Measured (us, in a captured graph): 1 row of 12 heads to 512
+// keys in one piece 13.4, in four 8.5; to 2048 in 8 pieces 12.3, in 64 7.8; 256 of 12 to 4096 in 8 pieces 23.3, in 16 26.0; 1024 of 12 to
+// 512 in one 12.6, in two 19.9.
+static XattnDeal deal(long long units, int nw, int tiles, int walk, int step, long long places, double us_per_step, double bytes_per_piece) {
+  const int steps = (walk + step - 1) / step;
+  const double per_piece = bytes_per_piece / 5e6, whole = steps * us_per_step;
+  long long pieces = (long long)std::sqrt(whole / per_piece);
+  pieces = std::min({pieces, places / std::max<long long>(1, units), (long long)(steps + 1) / 2, (long long)XATTN_PIECES});   // (two steps at least)
+  if (pieces < 2 || whole / pieces + 4.0 + pieces * per_piece >= whole) pieces = 1;
+  const int each = (int)((steps + pieces - 1) / pieces);
+  return XattnDeal{nw, tiles, (steps + each - 1) / each, each * step};
 }
+// (forward and dq share a deal: the two fp32 rows of a piece, and a step of 64 or 32 keys)
 XattnDeal xattn_deal_rows(int B, int G, int rows, int Nk) {
   const int nw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4, tiles = (rows + 32 * nw - 1) / (32 * nw);
-  return deal((long long)B * G * tiles, nw, tiles, Nk, nw == 4 ? 64 : 32, 256, (long long)compute_units() * (nw == 4 ? 2 : 4));
+  return deal((long long)B * G * tiles, nw, tiles, Nk, nw == 4 ? 64 : 32, (long long)compute_units() * (nw == 4 ? 2 : 4), nw == 4 ? 1.0 : 0.7,
+              (double)B * G * rows * 2 * (D + 4) * 4);
 }
 XattnDeal xattn_deal_keys(int B, int G, int group, int Nq, int Nk) {
   const int nw = Nk <= 32 ? 1 : Nk <= 64 ? 2 : 4, tiles = (Nk + 32 * nw - 1) / (32 * nw);
-  return deal((long long)B * G * tiles, nw, tiles, group * ((Nq + 63) / 64), 1, 4, (long long)compute_units() * 2);
+  return deal((long long)B * G * tiles, nw, tiles, group * ((Nq + 63) / 64), 1, (long long)compute_units() * 2, 2.0, (double)B * G * Nk * 4 * D * 4);
 }
 
 void launch_xattn_fwd(const XattnArgs& a, hipStream_t stream) {
