@@ -210,6 +210,14 @@ def test_norm_quantised_for_a_linear_layer(M, K, with_res):
     assert np.abs(codes).max() == 127
 
 
+@pytest.mark.parametrize("M", [2, 5, 200])
+def test_norm_quantised_without_a_weight(M):
+    x = _bf16(np.random.default_rng(M), (M, 640), 2.0).cuda()
+    ones = torch.ones(640, dtype=torch.bfloat16, device="cuda")
+    a, b = (_codes(sla.w8a8_norm_quantize_act(x, w)[0], M, 640) for w in (None, ones))
+    assert all((u == v).all() for u, v in zip(a, b))
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 256, 512), (130, 384, 1536), (1500, 1536, 640)])
 def test_norm_linear(M, N, K):
     r = np.random.default_rng([M, N, K])
