@@ -22,7 +22,8 @@ int xattn_problem(int B, int H, int Hkv, int Nq, int Nk, int d, double scale, Xa
   a->rows = a->group * Nq;
   a->scale = (float)(scale == 0.0 ? 1.0 / sqrt((double)D) : scale);
   a->c2 = (float)((scale == 0.0 ? 1.0 / sqrt((double)D) : scale) * 1.4426950408889634);
-  a->fwd = a->dqd = xattn_deal_rows(B, Hkv, a->rows, Nk);
+  a->fwd = xattn_deal_rows(B, Hkv, a->rows, Nk, true);
+  a->dqd = xattn_deal_rows(B, Hkv, a->rows, Nk, false);
   a->dkv = xattn_deal_keys(B, Hkv, a->group, Nq, Nk);
   return SLA_OK;
 }

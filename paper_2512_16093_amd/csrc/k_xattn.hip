@@ -16,6 +16,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "tiles.h"
 #include "xattn.h"
@@ -54,8 +55,9 @@ struct AlignedCopy : TileCopy<WAVES> {
       for (int i = 0; i < this->PPW; ++i) copy_piece(i < 4 ? b : b + 16 * this->snb, this->off[i & 3], to + i * 1024);
       return;
     }
-    int ln = this->lane;
+    int ln = threadIdx.x;
     asm volatile("" : "+v"(ln));              // (nothing of this path is worth a register outside of it)
+    ln &= 63;
 #pragma unroll 1
     for (int i = 0; i < this->PPW; ++i) {
       const int r = 4 * (this->PPW * this->w + i) + (ln >> 4);
@@ -116,11 +118,24 @@ __device__ __forceinline__ void store_partial(float* row, const v16f (&x)[4], in
       *(float4*)(row + 32 * ct + 8 * g + 4 * hf) = float4{x[ct][4 * g], x[ct][4 * g + 1], x[ct][4 * g + 2], x[ct][4 * g + 3]};
 }
 
+// s plus both halves of a word of bf16 numbers.
+__device__ __forceinline__ float bf16_pair_sum(uint32_t w, float s) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, w), __builtin_bit_cast(v2bf, 0x3F803F80u), s, false);
+}
+
 // LSE: the log-sum-exp is wanted too (of the unrounded weights: its own sum).  SPLIT: a piece of the walk, to the workspace.
+//
+// A step is 32 keys: 8 KiB each of K and V in one half of a ring of two.  Kept to 168 registers and 32 KiB, so that three wavefronts
+// share a SIMD: one issues products, one its exponentials, one waits for its queries or for its rows to leave.  With 64 keys a step
+// (224 registers, 64 KiB, two wavefronts): 12 x 32760 queries to 64 keys 39.0 us, now 37.7, to 512 116 / 106, to 8192 1447 / 1405; 40 x
+// 75600 to 512 911 / 842.  For that the operands come in one stream of LDS reads, three ahead of their products (K as rows, then V
+// transposed), the weights are summed on the vector ALU (a product with ones took 16 registers and one in nine of the matrix
+// instructions), and whole walks take two steps a turn, so that the halves of the ring are constants and the addresses of the reads
+// are formed once; the last steps, where a key may not exist, and pieces of a walk go through a body of their own.
 template <int NW, bool LSE, bool SPLIT>
-__global__ void __launch_bounds__(NW * 64, 2) xattn_fwd_kernel(XattnArgs a) {
-  constexpr int KT = NW == 4 ? 2 : 1, STEP_B = 2 * KT * SWZ_TILE_B, STEP = 32 * KT;
-  __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];   // two steps' tiles: KT of K, then KT of V
+__global__ void __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) xattn_fwd_kernel(XattnArgs a) {
+  constexpr int DEEP = 3, STEP = 32, STEP_B = 2 * SWZ_TILE_B;
+  __shared__ __attribute__((aligned(16))) unsigned char ring[2 * STEP_B];   // two steps' tiles, of K, then of V
   unsigned unit;
   if (!xattn_unit((unsigned)a.G * a.fwd.splits * a.fwd.tiles, a.B, unit)) return;
   const int rest = unit / (unsigned)a.fwd.tiles, tile = unit - (unsigned)rest * a.fwd.tiles;
@@ -128,14 +143,13 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_fwd_kernel(XattnArgs a) {
   const int b = (unsigned)bg / (unsigned)a.G, g = bg - b * a.G;
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
   const int len = xattn_len(a, b), k0 = SPLIT ? split * a.fwd.chunk : 0, k1 = SPLIT ? min(len, k0 + a.fwd.chunk) : len;
-  const int r0 = (tile * NW + w) * 32, row = r0 + l32;
+  const int r0 = (tile * NW + w) * 32;
   uint4 qf[8];
-  query_operands(a.q, QueryRows(a, a.lq, b, g), row, a.rows, hf, qf);
+  query_operands(a.q, QueryRows(a, a.lq, b, g), r0 + l32, a.rows, hf, qf);
   v16f o[4];
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct) o[ct] = v16f{};
-  float m = -FLT_MAX, lx = 0.f;
-  v16f lacc = v16f{};    // register 0: the running sum of the rounded weights
+  float m = -FLT_MAX, l = 0.f, lx = 0.f;       // l: the running sum of the rounded weights of this lane's keys
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
   if (k0 < k1) {
     AlignedCopy<NW> ck, cv;
@@ -143,93 +157,100 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_fwd_kernel(XattnArgs a) {
     cv.init(a.v + b * a.lv.sb + g * a.lv.sh, a.lv.sn, w, lane);
     const int n_off = swz_lane_offset(l32, hf), t_off = swz_tr_lane_offset(lane);
     auto request = [&](int key0, int half) __attribute__((always_inline)) {
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
-        ck.tile(key0 + 32 * kt, len, lds0 + half * STEP_B + kt * SWZ_TILE_B);
-        cv.template tile<true>(key0 + 32 * kt, len, lds0 + half * STEP_B + (KT + kt) * SWZ_TILE_B);   // (zero times what lies there need not be zero)
-      }
+      ck.tile(key0, len, lds0 + half * STEP_B);
+      cv.template tile<true>(key0, len, lds0 + half * STEP_B + SWZ_TILE_B);   // (zero times what lies behind the last key need not be zero)
     };
     request(k0, 0);
-    int half = 0;
-    for (int key0 = k0; key0 < k1; key0 += STEP, half ^= 1) {
+    // `half`: of the ring, a constant or not; whole: every key of the step exists
+    auto step = [&](int key0, auto half, auto whole) __attribute__((always_inline)) {
+      constexpr bool FIXED = !std::is_same<decltype(half), int>::value;
       copies_barrier<0>();                     // this step's tiles have landed; those of the step before are consumed
       if (key0 + STEP < k1) request(key0 + STEP, half ^ 1);
-      int no = n_off + half * STEP_B, to = t_off + half * STEP_B;
-      asm volatile("" : "+v"(no), "+v"(to));
-      v16f s[KT];
-      float mx = -INFINITY;
-      uint4 ak[8], tv[2][4];
+      const unsigned char* mine = ring + (FIXED ? half * STEP_B : 0);
+      int no = n_off + (FIXED ? 0 : half * STEP_B), to = t_off + (FIXED ? 0 : half * STEP_B);
+      if constexpr (!FIXED) asm volatile("" : "+v"(no), "+v"(to));
+      auto operand = [&](int i) __attribute__((always_inline)) {
+        return i < 8 ? n_op_swz(mine, no, i) : t_op_swz(mine + SWZ_TILE_B, to, i & 3, (i - 8) >> 2);
+      };
+      uint4 op[DEEP];
 #pragma unroll
-      for (int ks = 0; ks < 8; ++ks) ak[ks] = n_op_swz(ring, no, ks);
+      for (int i = 0; i < DEEP; ++i) op[i] = operand(i);
       __builtin_amdgcn_sched_barrier(0);
+      v16f s = v16f{};
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
-        s[kt] = v16f{};
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {       // behind a product: the read of the next tile's operand, at the end V's first ones
-          s[kt] = mfma_bf16(ak[ks], qf[ks], s[kt]);
-          if (kt + 1 < KT) ak[ks] = n_op_swz(ring + (kt + 1) * SWZ_TILE_B, no, ks);
-          else if (ks >= 4) tv[0][ks - 4] = t_op_swz(ring + KT * SWZ_TILE_B, to, ks - 4, 0);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+      for (int i = 0; i < 8; ++i) {
+        s = mfma_bf16(op[i % DEEP], qf[i], s);
+        op[i % DEEP] = operand(i + DEEP);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (!decltype(whole)::value) {
+        const int left = k1 - key0 - 4 * hf;
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
-        if (key0 + 32 * kt + 32 > k1) {        // (uniform) the last tile can hold keys that do not exist
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (key0 + 32 * kt + 8 * (r >> 2) + 4 * hf + (r & 3) >= k1) s[kt][r] = -INFINITY;
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kt][r]);
+        for (int r = 0; r < 16; ++r)
+          if (8 * (r >> 2) + (r & 3) >= left) s[r] = -INFINITY;
       }
-      // The reference m moves only when the tiles' maximum exceeds it by more than 2^8: the weights then stay below 2^8
+      float mx = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+      // The reference m moves only when the step's maximum exceeds it by more than 2^8: the weights then stay below 2^8
       // (harmless in bf16 and fp32) and the accumulators are rescaled a few times per row instead of every step.
       if (__any(mx * a.c2 > m + 8.0f)) {
         mx = fmaxf(mx, partner_f32(mx)) * a.c2;
         const float m_new = mx > m + 8.0f ? mx : m;
         const float alpha = __builtin_amdgcn_exp2f(m - m_new);
         m = m_new;
-        lacc[0] *= alpha;
+        l *= alpha;
         if constexpr (LSE) lx *= alpha;
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
       }
-      auto weight = [&](int e) __attribute__((always_inline)) {   // of element e % 16 of tile e / 16
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], a.c2, -m));
-        s[e >> 4][e & 15] = p;
-        if constexpr (LSE) lx += p;
+      auto weight = [&](int r) __attribute__((always_inline)) {
+        s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c2, -m));
+        if constexpr (LSE) lx += s[r];
       };
-      const uint4 ones = uint4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};  // bf16 1.0: sums the weights over the keys
 #pragma unroll
-      for (int e = 0; e < 8; ++e) weight(e);
+      for (int r = 0; r < 8; ++r) weight(r);
 #pragma unroll
-      for (int u = 0; u < 2 * KT; ++u) {       // 16 keys; behind their products the next ones' exponentials and operand reads
-        const uint4 pb = acc_operand(s[u >> 1], u & 1);
+      for (int u = 0; u < 2; ++u) {            // 16 keys; behind the first ones' products the others' exponentials
+        const uint4 pb = acc_operand(s, u);
+        l = bf16_pair_sum(pb.w, bf16_pair_sum(pb.z, bf16_pair_sum(pb.y, bf16_pair_sum(pb.x, l))));
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct) {
-          o[ct] = mfma_bf16(tv[u & 1][ct], pb, o[ct]);
-          if (u + 1 < 2 * KT) {
-            tv[(u + 1) & 1][ct] = t_op_swz(ring + (KT + ((u + 1) >> 1)) * SWZ_TILE_B, to, ct, (u + 1) & 1);
-            weight(8 * u + 8 + 2 * ct);
-            weight(8 * u + 9 + 2 * ct);
+          const int i = 8 + 4 * u + ct;
+          o[ct] = mfma_bf16(op[i % DEEP], pb, o[ct]);
+          if (i + DEEP < 16) op[i % DEEP] = operand(i + DEEP);
+          if (u == 0) {
+            weight(8 + 2 * ct);
+            weight(9 + 2 * ct);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
-        lacc = mfma_bf16(ones, pb, lacc);
+      }
+    };
+    int key0 = k0;
+    if constexpr (!SPLIT) {
+      for (; key0 + 2 * STEP <= k1; key0 += 2 * STEP) {
+        step(key0, std::integral_constant<int, 0>{}, std::true_type{});
+        step(key0 + STEP, std::integral_constant<int, 1>{}, std::true_type{});
       }
     }
+#pragma unroll 1
+    for (int half = 0; key0 < k1; key0 += STEP, half ^= 1) step(key0, half, std::false_type{});
   }
-  const float l = lacc[0];                     // (0: no key)
+  // (formed again: not worth registers through the walk)
+  int th = threadIdx.x;
+  asm volatile("" : "+v"(th));
+  const int ln = th & 63, upper = ln >> 5, row = r0 + (ln & 31);
+  l += partner_f32(l);                         // (0: no key)
   if constexpr (LSE) lx += partner_f32(lx);
   const long long first = ((long long)b * a.H + g * a.group) * a.Nq;   // of this key head's query rows among all
   if constexpr (SPLIT) {
     if (row < a.rows) {
       const long long at = (long long)split * a.B * a.H * a.Nq + first + row;
-      if (hf == 0) *(float4*)(a.part_ml + 4 * at) = float4{m, l, LSE ? lx : l, 0.f};
-      store_partial(a.part_o + at * D, o, hf);
+      if (upper == 0) *(float4*)(a.part_ml + 4 * at) = float4{m, l, LSE ? lx : l, 0.f};
+      store_partial(a.part_o + at * D, o, upper);
     }
   } else {
     const float inv = l > 0.f ? 1.0f / l : 0.f;
@@ -238,10 +259,10 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_fwd_kernel(XattnArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[ct][r] *= inv;
     if constexpr (LSE) {
-      if (hf == 0 && row < a.rows) a.lse[first + row] = l > 0.f ? (m + __builtin_amdgcn_logf(lx)) * LN2 : -INFINITY;
+      if (upper == 0 && row < a.rows) a.lse[first + row] = l > 0.f ? (m + __builtin_amdgcn_logf(lx)) * LN2 : -INFINITY;
     }
     copies_barrier<0>();                       // nobody reads the last step's tiles any more
-    store_query_rows(ring + w * 8192, o, lane, a.out, QueryRows(a, a.lo, b, g), r0, a.rows);
+    store_query_rows(ring + w * 8192, o, ln, a.out, QueryRows(a, a.lo, b, g), r0, a.rows);
   }
 }
 
@@ -404,9 +425,10 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
           dp = mfma_bf16(n_op_swz(tv, no, ks), df[ks], dp);
         }
         if (key0 + 32 * kt + 32 > k1) {
+          const int left = k1 - key0 - 32 * kt - 4 * hf;
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (key0 + 32 * kt + 8 * (r >> 2) + 4 * hf + (r & 3) >= k1) s[r] = -INFINITY;
+            if (8 * (r >> 2) + (r & 3) >= left) s[r] = -INFINITY;
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c2, -lse2)) * dp[r];
@@ -617,11 +639,11 @@ static XattnDeal deal(long long units, int nw, int tiles, int walk, int step, lo
   const int each = (int)((steps + pieces - 1) / pieces);
   return XattnDeal{nw, tiles, (steps + each - 1) / each, each * step};
 }
-// (forward and dq share a deal: the two fp32 rows of a piece, and a step of 64 or 32 keys)
-XattnDeal xattn_deal_rows(int B, int G, int rows, int Nk) {
-  const int nw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4, tiles = (rows + 32 * nw - 1) / (32 * nw);
-  return deal((long long)B * G * tiles, nw, tiles, Nk, nw == 4 ? 64 : 32, (long long)compute_units() * (nw == 4 ? 2 : 4), nw == 4 ? 1.0 : 0.7,
-              (double)B * G * rows * 2 * (D + 4) * 4);
+XattnDeal xattn_deal_rows(int B, int G, int rows, int Nk, bool fwd) {
+  const int nw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4, tiles = (rows + 32 * nw - 1) / (32 * nw), wide = nw == 4;
+  // places: three (forward) or two (dq) workgroups of four wavefronts to a compute unit, or four of fewer
+  return deal((long long)B * G * tiles, nw, tiles, Nk, fwd || !wide ? 32 : 64, (long long)compute_units() * (!wide ? 4 : fwd ? 3 : 2),
+              !wide ? 0.7 : fwd ? 0.5 : 1.6, (double)B * G * rows * 2 * (D + 4) * 4);
 }
 XattnDeal xattn_deal_keys(int B, int G, int group, int Nq, int Nk) {
   const int nw = Nk <= 32 ? 1 : Nk <= 64 ? 2 : 4, tiles = (Nk + 32 * nw - 1) / (32 * nw);

@@ -26,7 +26,7 @@ struct XattnArgs {
   float *part_dq, *part_dk, *part_dv;   // fp32 [splits, ...]
 };
 __host__ __device__ inline int xattn_padded_rows(int Nq) { return (Nq + 63) / 64 * 64; }
-XattnDeal xattn_deal_rows(int B, int G, int rows, int Nk);            // forward, dq
+XattnDeal xattn_deal_rows(int B, int G, int rows, int Nk, bool fwd);  // forward, or dq
 XattnDeal xattn_deal_keys(int B, int G, int group, int Nq, int Nk);   // dk, dv
 void launch_xattn_fwd(const XattnArgs& a, hipStream_t stream);
 void launch_xattn_bwd(const XattnArgs& a, hipStream_t stream);
