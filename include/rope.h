@@ -15,8 +15,8 @@
  *        to axis 2; pair number i of an axis of n turns by a = position theta^(-i / n).
  *
  * Everything is computed in fp32 and rounded once to bf16 (nearest even).  The angle is formed in
- * 64-bit fixed point (turns modulo 1), so that it is as exact at position 2^31 - 1 as at 1: its
- * error is below 2^-31 turns.
+ * 64-bit fixed point (turns modulo 1), so that it is good at position 2^31 - 1 as well as at 1: its
+ * error is below 2^-28 turns.
  *
  * Rules as in sla.h: every tensor pointer is a DEVICE pointer owned by the caller; the plan and the
  * strides are HOST structs read during the call; the library allocates nothing and never

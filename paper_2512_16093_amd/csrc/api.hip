@@ -262,7 +262,7 @@ BwdWorkspace make_bwd_workspace(const Problem& p, const Workspace& W) {
 #pragma GCC visibility push(default)
 extern "C" {
 
-int sla_version(void) { return 100; }
+int sla_version(void) { return 200; }
 
 const char* sla_status_string(int status) {
   switch (status) {

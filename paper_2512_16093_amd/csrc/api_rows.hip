@@ -64,12 +64,17 @@ int rope_make_plan(const int32_t pairs[3], const double theta[3], int pairing, r
   if (pairing != ROPE_INTERLEAVED && pairing != ROPE_HALVES) return SLA_ERR_UNSUPPORTED;
   const long double turn = 6.283185307179586476925286766559005768L;
   int j = 0;
-  for (int ax = 0; ax < 3; ++ax)
-    for (int i = 0; i < pairs[ax]; ++i, ++j) {
-      // (at most 1 / 2 pi: below one turn a step)
-      plan->turns[j] = (uint64_t)roundl(ldexpl(powl((long double)theta[ax], -(long double)i / pairs[ax]) / turn, 64));
+  for (int ax = 0; ax < 3; ++ax) {
+    const int n = pairs[ax];
+    // theta^(-i / n) from the i-th root's powers, by squaring: 64 bits each, at most 2^-58 off in the last of 64
+    long double power[D / 2] = {1.0L};
+    const long double root = n > 1 ? powl((long double)theta[ax], -1.0L / n) : 1.0L;
+    for (int i = 1; i < n; ++i) power[i] = power[i / 2] * power[i / 2] * ((i & 1) ? root : 1.0L);
+    for (int i = 0; i < n; ++i, ++j) {
+      plan->turns[j] = (uint64_t)(power[i] / turn * 18446744073709551616.0L + 0.5L);   // (at most 1 / 2 pi: below one turn a step)
       plan->axis[j] = (uint8_t)ax;
     }
+  }
   plan->pairing = pairing;
   plan->made = PLAN_MADE;
   return SLA_OK;

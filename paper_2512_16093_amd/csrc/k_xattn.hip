@@ -345,6 +345,10 @@ __global__ void __launch_bounds__(256) xattn_join_kernel(XattnArgs a) {
 }
 
 // ---------------------------------------------------------------------------
+// dS = P o (dO V^T - delta) with P = 2^(S - lse), dQ = scale dS K: three products of a tile pair, S and dP formed again rather than
+// kept (a matrix of 400 MB at 12 x 32760 x 512).  P and dS are fp32 until dS is rounded to the bf16 operand of the last product.
+// Two wavefronts per SIMD (q, dO and dQ alone are 128 registers); 12 x 32760 queries to 512 keys 182 us (0.85 PFLOP/s, 400 MB), at
+// longer walks 1.2 PFLOP/s: power.  Operands read four products ahead in a fixed order: 181.
 template <int NW, bool SPLIT>
 __global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
   constexpr int KT = NW == 4 ? 2 : 1, STEP_B = 2 * KT * SWZ_TILE_B, STEP = 32 * KT;
@@ -454,7 +458,10 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
   }
 }
 
-// A wavefront owns 32 keys and walks over the query rows of every head of its group, 32 QT rows a step.
+// dV = P^T dO, dK = scale dS^T Q.  A wavefront owns 32 keys and walks over the query rows of every head of its group, 32 QT rows
+// a step; P and dS are rounded to bf16 as operands, the sums stay in fp32 in registers (and in the workspace, where a walk is split:
+// few key blocks have to fill the chip, and their pieces are added up in a fixed order).  12 x 32760 queries to 512 keys, ten pieces: 205
+// us, 1.0 PFLOP/s, the matrix pipe 48 % busy, power; with one wavefront per SIMD and the compiler's order 348.
 template <int NW, bool SPLIT>
 __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) xattn_dkv_kernel(XattnArgs a) {
   constexpr int QT = 2, STEP_B = 2 * QT * SWZ_TILE_B + 512, STEP = 32 * QT, DEEP = 2;  // Q, dO, then lse2 and -delta of the rows
@@ -600,7 +607,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) xattn_dkv_kernel(Xat
   }
 }
 
-// to[b][h][n] = sum over s of part[s][b][h][n], eight rows per workgroup; blockIdx.y: which of two tensors.
+// to[b][h][n] = sum over s of part[s][b][h][n], in the order of s, eight rows per workgroup; blockIdx.y: which of two tensors.
 struct XattnSum {
   const float* part[2];
   bf16_t* to[2];

@@ -4,6 +4,7 @@ import ctypes
 import os
 import re
 
+import numpy as np
 import pytest
 import torch
 
@@ -38,6 +39,16 @@ def test_plans():
     for j, (base, i, n) in enumerate([(10000.0, i, 22) for i in range(22)] + [(10000.0, i, 21) for i in range(21)] +
                                      [(500.0, i, 21) for i in range(21)]):
         assert abs(p.turns[j] * 2.0 ** -64 * 6.283185307179586 - base ** (-i / n)) < 1e-15
+    # at the farthest position the angle is off by less than 2^-28 turns, whatever the base
+    turn = 2 * np.longdouble("3.14159265358979323846264338327950288")
+    for pairs in ((64, 0, 0), (1, 62, 1), (10, 20, 34)):
+        for base in (1.0, 1.0000001, 1.5, 500.0, 1e12):
+            p, j = sla.rope_make_plan(pairs, base), 0
+            for n in pairs:
+                for i in range(n):
+                    want = np.longdouble(base) ** (-np.longdouble(i) / n) / turn
+                    assert abs(float(np.longdouble(p.turns[j]) / np.longdouble(2) ** 64 - want)) * 2 ** 31 < 2 ** -28, (pairs, base, i)
+                    j += 1
     L = sla.lib()
     out = sla.RopePlan()
 
