@@ -1,7 +1,7 @@
 // Root-mean-square norm with the residual's addition (include/norm.h), forward and backward; its first half for the norm in
 // front of a W8A8 Linear layer (include/w8a8.h), whose second half is the quantisation (k_w8a8.hip).
 //
-// A team of T threads per row: a wavefront up to 2048 features, a workgroup of 256 up to 8192, of 1024 up to 16384.  The row stays
+// A team of T threads per row: a wavefront up to 2048 features, a workgroup of 256 to 512 up to 8192, of 1024 up to 16384.  The row stays
 // in registers between the sum of its squares and its result, so every tensor is read or written once: bound by HBM.
 #include "rows.h"
 
@@ -12,7 +12,7 @@ __device__ __forceinline__ uint4 load_row(const bf16_t* row, int e) { return loa
 
 // STATS: h and r instead of h and y.
 template <int T, int CH, bool STATS, bool NT>
-__global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_fwd_kernel(const bf16_t* __restrict__ x, const bf16_t* __restrict__ res,
+__global__ void __launch_bounds__(T == 64 ? 256 : T) norm_fwd_kernel(const bf16_t* __restrict__ x, const bf16_t* __restrict__ res,
                                                                          const bf16_t* __restrict__ weight, bf16_t* __restrict__ h,
                                                                          bf16_t* __restrict__ y, float* __restrict__ r_out, int M, int K,
                                                                          float eps) {
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_fwd_kernel(const 
 
 // dx, and each workgroup's share of dw in registers over the rows it takes.
 template <int T, int CH, bool NT>
-__global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_bwd_kernel(const bf16_t* __restrict__ dy, const bf16_t* __restrict__ dh,
+__global__ void __launch_bounds__(T == 64 ? 256 : T) norm_bwd_kernel(const bf16_t* __restrict__ dy, const bf16_t* __restrict__ dh,
                                                                          const bf16_t* __restrict__ h, const bf16_t* __restrict__ weight,
                                                                          bf16_t* __restrict__ dx, float* __restrict__ part, int M, int K,
                                                                          float eps) {
@@ -181,7 +181,9 @@ __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_bwd_kernel(const 
 }
 
 // ---------------------------------------------------------------------------
-// The team and the shares of a thread for K features: F(T, CH).
+// The team and the shares of a thread for K features: F(T, CH).  In the forward direction threads are fitted to two shares each (with
+// 256 threads of three for 5120 features, a sixth of them idle, 75600 rows took 529 us, now 518; 6144 160 / 156); the gradient, whose
+// threads hold sums of dw too, takes three of 256 threads there (568 us; with 320 586; 6144 184 / 207), but two of 512 for 8192 (265 / 231).
 #define NORM_TEAMS(K, F)                  \
   do {                                    \
     const int n_ = (K) / 8;               \
@@ -190,8 +192,21 @@ __global__ void __launch_bounds__(T == 1024 ? 1024 : 256) norm_bwd_kernel(const 
     else if (n_ <= 192) F(64, 3);         \
     else if (n_ <= 256) F(64, 4);         \
     else if (n_ <= 512) F(256, 2);        \
+    else if (n_ <= 640) F(320, 2);        \
+    else if (n_ <= 768) F(384, 2);        \
+    else if (n_ <= 1024) F(512, 2);       \
+    else F(1024, 2);                      \
+  } while (0)
+#define NORM_BWD_TEAMS(K, F)              \
+  do {                                    \
+    const int n_ = (K) / 8;               \
+    if (n_ <= 64) F(64, 1);               \
+    else if (n_ <= 128) F(64, 2);         \
+    else if (n_ <= 192) F(64, 3);         \
+    else if (n_ <= 256) F(64, 4);         \
+    else if (n_ <= 512) F(256, 2);        \
     else if (n_ <= 768) F(256, 3);        \
-    else if (n_ <= 1024) F(256, 4);       \
+    else if (n_ <= 1024) F(512, 2);       \
     else F(1024, 2);                      \
   } while (0)
 
@@ -205,7 +220,7 @@ void launch_norm_fwd(const void* x, const void* res, const void* w, void* h, voi
     if (streams(M, K, res ? 4 : 2)) NORM_FWD_(T, CH, true); else NORM_FWD_(T, CH, false);                                 \
   } while (0)
 #define NORM_FWD_(T, CH, NT)                                                                                              \
-  norm_fwd_kernel<T, CH, false, NT><<<row_workgroups(M, T), T == 1024 ? 1024 : 256, 0, stream>>>(                         \
+  norm_fwd_kernel<T, CH, false, NT><<<row_workgroups(M, T), T == 64 ? 256 : T, 0, stream>>>(                         \
       (const bf16_t*)x, (const bf16_t*)res, (const bf16_t*)w, (bf16_t*)h, (bf16_t*)y, nullptr, M, K, eps)
   NORM_TEAMS(K, NORM_FWD);
 #undef NORM_FWD_
@@ -217,7 +232,7 @@ void launch_norm_stats(const void* x, const void* res, void* h, float* r, int M,
     if (res && streams(M, K, 3)) NORM_STATS_(T, CH, true); else NORM_STATS_(T, CH, false);                                \
   } while (0)
 #define NORM_STATS_(T, CH, NT)                                                                                            \
-  norm_fwd_kernel<T, CH, true, NT><<<row_workgroups(M, T), T == 1024 ? 1024 : 256, 0, stream>>>(                          \
+  norm_fwd_kernel<T, CH, true, NT><<<row_workgroups(M, T), T == 64 ? 256 : T, 0, stream>>>(                          \
       (const bf16_t*)x, (const bf16_t*)res, nullptr, (bf16_t*)h, nullptr, r, M, K, eps)
   NORM_TEAMS(K, NORM_STATS);
 #undef NORM_STATS_
@@ -240,9 +255,9 @@ void launch_norm_bwd(const void* dy, const void* dh, const void* h, const void* 
     if (streams(M, K, dh ? 4 : 3)) NORM_BWD_(T, CH, true); else NORM_BWD_(T, CH, false);                                  \
   } while (0)
 #define NORM_BWD_(T, CH, NT)                                                                                              \
-  norm_bwd_kernel<T, CH, NT><<<grid, T == 1024 ? 1024 : 256, 0, stream>>>((const bf16_t*)dy, (const bf16_t*)dh, (const bf16_t*)h, \
+  norm_bwd_kernel<T, CH, NT><<<grid, T == 64 ? 256 : T, 0, stream>>>((const bf16_t*)dy, (const bf16_t*)dh, (const bf16_t*)h, \
                                                                          (const bf16_t*)w, (bf16_t*)dx, part, M, K, eps)
-  NORM_TEAMS(K, NORM_BWD);
+  NORM_BWD_TEAMS(K, NORM_BWD);
 #undef NORM_BWD_
 #undef NORM_BWD
   PartialSums s{};

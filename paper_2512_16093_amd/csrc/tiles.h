@@ -68,8 +68,8 @@ struct TileCopy {
     }
   }
   // For copies of several pieces with immediate offsets: piece i reads base3 + off3(i) + 1024 i.
-  __device__ __forceinline__ const char* base3(int row0) const { return slice + row0 * snb - 3072; }
-  __device__ __forceinline__ unsigned off3(int i) const { return off[i] + (3072 - 1024 * i); }
+  __device__ __forceinline__ const char* base3(int row0) const { return slice + row0 * snb - 3 * 1024; }
+  __device__ __forceinline__ unsigned off3(int i) const { return off[i] + (3 - i) * 1024; }
   __device__ __forceinline__ unsigned dst(unsigned lds_tile) const { return __builtin_amdgcn_readfirstlane(lds_tile + w * PPW * 1024); }
   // Are rows row0 .. row0 + rows - 1 whole, and their copies of the plain kind?  (uniform)
   __device__ __forceinline__ bool plain(int row0, int rows, int N) const { return row0 + rows <= N && odd == 0; }
