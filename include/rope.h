@@ -18,6 +18,9 @@
  * 64-bit fixed point (turns modulo 1), so that it is good at position 2^31 - 1 as well as at 1: its
  * error is below 2^-28 turns.
  *
+ * With a norm the mean of the squares has to stay within fp32 (|x| below 1e19): beyond, the heads or tokens
+ * concerned come out zero or NaN.
+ *
  * Rules as in sla.h: every tensor pointer is a DEVICE pointer owned by the caller; the plan and the
  * strides are HOST structs read during the call; the library allocates nothing and never
  * synchronises; work is enqueued on `stream`; inputs are never written; outputs must not alias
