@@ -9,7 +9,7 @@
  *
  * Query heads may share key heads: head h of H reads head h / (H / Hkv) of Hkv.  A sample without keys
  * gives zeros and lse = -infinity.  What lies in keys and values behind k_lens[b] is not used, whatever it is
- * (NaN and infinities included).
+ * (NaN and infinities included); a NaN in a query or in a key that is used makes the rows that meet it NaN, in out and in lse.
  * The products run in bf16 on the matrix cores with fp32 accumulation, softmax and its statistics in
  * fp32; the weights are rounded to bf16 for the product with V, and divided by the sum of the ROUNDED
  * weights; lse is that of the unrounded ones.

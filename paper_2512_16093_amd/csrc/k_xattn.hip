@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) xattn_fwd_kernel(Xat
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[ct][r] *= inv;
     if constexpr (LSE) {
-      if (upper == 0 && row < a.rows) a.lse[first + row] = l > 0.f ? (m + __builtin_amdgcn_logf(lx)) * LN2 : -INFINITY;
+      if (upper == 0 && row < a.rows) a.lse[first + row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(lx)) * LN2;   // (a NaN is not "no key")
     }
     copies_barrier<0>();                       // nobody reads the last step's tiles any more
     store_query_rows(ring + w * 8192, o, ln, a.out, QueryRows(a, a.lo, b, g), r0, a.rows);
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(256) xattn_join_kernel(XattnArgs a) {
   const long long bh = row / a.Nq;
   const int n = (int)(row - bh * a.Nq), b = (int)(bh / a.H), h = (int)(bh - (long long)b * a.H);
   *(uint2*)(a.out + b * a.lo.sb + h * a.lo.sh + n * a.lo.sn + 4 * c) = uint2{pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv)};
-  if (a.lse && c == 0) a.lse[row] = l > 0.f ? (M + __builtin_amdgcn_logf(lx)) * LN2 : -INFINITY;
+  if (a.lse && c == 0) a.lse[row] = l == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(lx)) * LN2;
 }
 
 // ---------------------------------------------------------------------------
