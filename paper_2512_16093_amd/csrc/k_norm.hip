@@ -128,7 +128,8 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) norm_bwd_kernel(const bf16_
 #pragma unroll
       for (int i = 0; i < T / 64; ++i) { ss += red[turn][0][i]; xg += red[turn][1][i]; }
     }
-    const float r = __builtin_amdgcn_rsqf(ss * inv + eps), dot = xg * inv * r * r * r;
+    // (dx = r (g - x r^2 mean(x g)): r^3 need not be a number of fp32, r is up to 1 / sqrt(eps))
+    const float r = __builtin_amdgcn_rsqf(ss * inv + eps), dot = xg * inv * r * r;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float x[8], g[8], gx[8], up[8];
@@ -137,7 +138,7 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) norm_bwd_kernel(const bf16_
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         dw[c][i] = __builtin_fmaf(gx[i], r, dw[c][i]);
-        up[i] += __builtin_fmaf(g[i], r, -x[i] * dot);
+        up[i] = __builtin_fmaf(__builtin_fmaf(-x[i], dot, g[i]), r, up[i]);
       }
       if (t + c * T < n) store_to<NT>(dx + m * K + 8ll * (t + c * T), pack8(up));
     }

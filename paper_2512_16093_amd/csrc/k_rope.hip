@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(256) rope_bwd_kernel(RopeArgs a) {
         xg = red2[turn][1][0] + red2[turn][1][1] + red2[turn][1][2] + red2[turn][1][3];
       }
       r = __builtin_amdgcn_rsqf(ss * inv + a.eps);
-      dot = xg * inv * r * r * r;
+      dot = xg * inv * r * r;            // (dx = r (w g - x r^2 mean(x w g)): r^3 need not be a number of fp32)
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -246,15 +246,15 @@ __global__ void __launch_bounds__(256) rope_bwd_kernel(RopeArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) xg = __builtin_fmaf(xl[j] * wl[j], gl[j], __builtin_fmaf(xh[j] * wh[j], gh[j], xg));
           r = __builtin_amdgcn_rsqf(row_sum(pair_dot(xl, xh, xl, xh)) * inv + a.eps);
-          dot = row_sum(xg) * inv * r * r * r;
+          dot = row_sum(xg) * inv * r * r;
         }
         const int u = NORM == 1 ? 0 : c;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           dwl[u][j] = __builtin_fmaf(gl[j] * xl[j], r, dwl[u][j]);
           dwh[u][j] = __builtin_fmaf(gh[j] * xh[j], r, dwh[u][j]);
-          gl[j] = __builtin_fmaf(gl[j] * wl[j], r, -xl[j] * dot);
-          gh[j] = __builtin_fmaf(gh[j] * wh[j], r, -xh[j] * dot);
+          gl[j] = __builtin_fmaf(-xl[j], dot, gl[j] * wl[j]) * r;
+          gh[j] = __builtin_fmaf(-xh[j], dot, gh[j] * wh[j]) * r;
         }
       }
       if (head < x.H) put(head, gl, gh);
