@@ -18,8 +18,8 @@
  * sla_status; argument errors are found on the host before any launch.  Results are deterministic
  * (no floating-point atomics).
  * Tensors are bf16 [M, K], row-major and contiguous, 16-byte aligned (else SLA_ERR_LAYOUT).
- * Values are expected finite, and the mean of a row's squares within fp32 (|h| below 1e19): beyond, that row alone
- * comes out zero or NaN.
+ * Values are expected finite, and the sum of a row's squares within fp32 (|h| up to 1e17 is inside for every K):
+ * beyond, that row alone comes out zero or NaN.  In the backward pass the same holds of the sum of |h o w o dy|.
  * Supported: K a multiple of 8, 8 <= K <= 16384; 1 <= M <= 2^22; eps > 0 (else SLA_ERR_VALUE).
  */
 #ifndef NORM_H_

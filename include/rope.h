@@ -18,8 +18,9 @@
  * 64-bit fixed point (turns modulo 1), so that it is good at position 2^31 - 1 as well as at 1: its
  * error is below 2^-28 turns.
  *
- * With a norm the mean of the squares has to stay within fp32 (|x| below 1e19): beyond, the heads or tokens
- * concerned come out zero or NaN.
+ * With a norm the SUM of the squares that a mean is taken of has to stay within fp32 (|x| up to 1e17 is inside
+ * for every number of heads): beyond, the heads or tokens concerned come out zero or NaN.  In the backward pass
+ * the same holds of the sums of |x o w o g|.
  *
  * Rules as in sla.h: every tensor pointer is a DEVICE pointer owned by the caller; the plan and the
  * strides are HOST structs read during the call; the library allocates nothing and never

@@ -93,8 +93,8 @@ int w8a8_gemm_fwd(const void* workspace, size_t workspace_bytes, const void* wq,
  * All of them 16-byte aligned (else SLA_ERR_LAYOUT); K <= 16384 here; eps > 0 (else SLA_ERR_VALUE).
  * The workspace of w8a8_norm_workspace_bytes(M, K) bytes holds the quantised activations and the rows'
  * factors; behind w8a8_norm_quantize_act it is one that w8a8_gemm_fwd takes for the same M and K.
- * Values are expected finite, and the mean of a row's squares within fp32 (|h| below 1e19); others make that row
- * NaN or zero, and a NaN has no code: it is undefined which of its block's codes change. */
+ * Values are expected finite, and the sum of a row's squares within fp32 (|h| up to 1e17 is inside for every K);
+ * others make that row NaN or zero, and a NaN has no code: it is undefined which of its block's codes change. */
 size_t w8a8_norm_workspace_bytes(int M, int K);
 int w8a8_norm_quantize_act(const void* x, const void* res, const void* norm_w, void* h, int M, int K, double eps,
                            void* workspace, size_t workspace_bytes, sla_stream_t stream);

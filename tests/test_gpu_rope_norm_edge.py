@@ -58,3 +58,45 @@ def test_gradient_of_the_rotation_of_tiny_heads(H, norm, pairing):
     got = sla.rope_qk_bwd(dy.cuda(), None, p, plan, q=x.cuda(), q_weight=w.cuda(), norm=norm, eps=TINY_EPS)
     _near(got[0], dx, scale, "dx")
     assert torch.isfinite(got[2]).all()
+
+
+def _large(r, shape):
+    """Values up to 1e17, half of them of that size: what the headers promise of every width."""
+    x = 1e17 * r.choice((-1.0, 1.0), shape) * np.where(r.random(shape) < 0.5, 1.0, r.random(shape))
+    return torch.from_numpy((x * (1 - 2.0 ** -7)).astype(np.float32)).bfloat16()
+
+
+@pytest.mark.parametrize("M,K", [(3, 1024), (5, 5120), (2, 16384)])
+@pytest.mark.parametrize("with_res", [False, True])
+def test_norm_of_the_largest_values(M, K, with_res):
+    r = np.random.default_rng([M, K, 4])
+    x, w, dy = _large(r, (M, K)), (1 + 0.2 * _bf16(r, K)).bfloat16(), _bf16(r, (M, K))
+    res = (x.float() * -0.25).bfloat16() if with_res else None
+    h = x if res is None else (x.float() + res.float()).bfloat16()
+    rg = None if res is None else res.cuda()
+    n = bo.norm_fwd(_np(h), _np(w), 1e-6)
+    y, got_h = sla.norm_rms_fwd(x.cuda(), w.cuda(), rg)
+    assert torch.equal(got_h.cpu(), h)
+    _near(y, n, np.abs(n), "y")
+    dx, _, scale = bo.norm_bwd(_np(dy), _np(h), _np(w), None, 1e-6)
+    _near(sla.norm_rms_bwd(dy.cuda(), h.cuda(), w.cuda())[0], dx, scale, "dx")
+    ws, _ = sla.w8a8_norm_quantize_act(x.cuda(), w.cuda(), rg)
+    codes, scales = (_np(t) for t in sla.w8a8_debug_unpack(ws, False, M, K))
+    want = np.abs(n.reshape(M, K // 128, 128)).max((0, 2)) / 127
+    assert (np.abs(scales[0] - want) <= F32 * want).all()
+    assert (np.abs(codes - n / np.repeat(want, 128)) <= 0.5 + 127 * 2 * F32).all()
+
+
+@pytest.mark.parametrize("H,norm", [(3, "head"), (12, "token"), (64, "token"), (64, "head")])
+def test_rotation_of_the_largest_values(H, norm):
+    r = np.random.default_rng([H, 5])
+    x, w, dy = _large(r, (1, H, 5, 128)), (1 + 0.2 * _bf16(r, 128 if norm == "head" else H * 128)).bfloat16(), _bf16(r, (1, H, 5, 128))
+    pos = r.integers(0, 90, (1, 5, 3))
+    ang, p, plan = bo.angles(pos, (22, 21, 21), (10000.0,) * 3), torch.from_numpy(pos[0].astype(np.int32)).cuda(), sla.rope_make_plan()
+    want = bo.rope_fwd(_np(x), ang, "interleaved", _np(w), norm)
+    size = np.abs(bo.rope_fwd(_np(x), ang * 0, "interleaved", _np(w), norm))
+    y = sla.rope_qk_fwd(x.cuda(), None, p, plan, w.cuda(), norm=norm)[0]
+    _near(y, want, np.repeat(size[..., 0::2] + size[..., 1::2], 2, -1), "y")
+    dx, _, scale = bo.rope_bwd(_np(dy), _np(x), ang, "interleaved", _np(w), norm)
+    got = sla.rope_qk_bwd(dy.cuda(), None, p, plan, q=x.cuda(), q_weight=w.cuda(), norm=norm)
+    _near(got[0], dx, scale, "dx")
