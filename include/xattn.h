@@ -13,6 +13,9 @@
  * The products run in bf16 on the matrix cores with fp32 accumulation, softmax and its statistics in
  * fp32; the weights are rounded to bf16 for the product with V, and divided by the sum of the ROUNDED
  * weights; lse is that of the unrounded ones.
+ * |scale Q.K| up to 2^24 is inside what the forward pass takes: fp32 does not resolve larger scores to a unit, and
+ * from 2^31 / log2(e) on a row can come out NaN or as one without keys.  The backward pass forms its weights anew from lse, which is rounded
+ * to fp32: they are off by up to 2^-22 |lse| of their size, within a rounding to bf16 up to |lse| = 2^14.
  *
  * Rules as in sla.h: every tensor pointer is a DEVICE pointer owned by the caller, strides are HOST
  * structs; the library allocates nothing and never synchronises; work is enqueued on `stream`; scratch
@@ -22,8 +25,8 @@
  * sla_status; argument errors are found on the host before any launch.  Results are deterministic (no
  * floating-point atomics).
  * Supported: d == 128; H a multiple of Hkv; Nq, Nk >= 1; B H <= 65535; B H Nq and B Hkv Nk below 2^30;
- * 0 <= scale, finite (0: 1 / sqrt(d); else SLA_ERR_VALUE); strides as for sla_attention_fwd_strided (NULL =
- * contiguous; 16-byte aligned bases in either case, else SLA_ERR_LAYOUT).
+ * scale 0 (1 / sqrt(d)) or from 1e-30 to 1e30 (else SLA_ERR_VALUE); strides as for sla_attention_fwd_strided
+ * (NULL = contiguous; 16-byte aligned bases in either case, else SLA_ERR_LAYOUT).
  */
 #ifndef XATTN_H_
 #define XATTN_H_

@@ -1,8 +1,10 @@
-"""Attention to a sequence of another length: numbers that are none, in every way the walk over the keys is dealt out."""
+"""Attention to a sequence of another length at the ends of its range, in every way the walk over the keys is dealt out: numbers that
+are none, the largest scores."""
 import numpy as np
 import pytest
 import torch
 
+from oracle import block_oracle as bo
 from paper_2512_16093_amd import binding as sla
 
 pytestmark = pytest.mark.gpu
@@ -64,3 +66,29 @@ def test_nan_stays_nan(B, H, Hkv, Nq, Nk, lens, least, most):
         got, got_lse = sla.xattn_fwd(q, k, bad, k_lens=dl, want_lse=True)
         assert torch.equal(got_lse, lse)
         same_but(got, out, where)
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,lens,least,most", WALKS)
+def test_the_largest_scores(B, H, Hkv, Nq, Nk, lens, least, most):
+    """Scores of just below 2^24 either way, which fp32 holds exactly here (whole numbers), a few units apart where they count.
+    Tolerances: 3.1 roundings to bf16 of sum p |v| (test_gpu_xattn.py), and of the exponents, up to 7 log2(e) apart, what fp32 adds to
+    them (far below one); lse: the rounding of a number of its size, its two factors and its sum's, 2^-22 in all."""
+    r = np.random.default_rng([B, H, Nk])
+    q, k = torch.zeros((B, H, Nq, 128)), torch.zeros((B, Hkv, Nk, 128))
+    q[..., 3] = torch.from_numpy(r.choice((-1.0, 1.0), (B, H, Nq))) * 2.0 ** 14        # times 1020: 2^24 - 2^16
+    q[..., 77] = 1.0
+    k[..., 3] = torch.from_numpy(r.choice((1020.0, 1020.0, 1016.0, -1020.0), (B, Hkv, Nk)))
+    k[0, 0, :, 3] = 1020.0                                                             # (rows whose scores are all the lowest)
+    k[..., 77] = torch.from_numpy(r.integers(0, 8, (B, Hkv, Nk)).astype(np.float64))
+    q, k, v = q.bfloat16(), k.bfloat16(), _bf16(r, (B, Hkv, Nk, 128))
+    dl = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = sla.xattn_fwd(q.cuda(), k.cuda(), v.cuda(), k_lens=dl, scale=1.0, want_lse=True)
+    args = [_np(t) for t in (q, k, v)]
+    want, want_lse = bo.xattn_fwd(*args, lens, 1.0)
+    size = bo.xattn_fwd(args[0], args[1], np.abs(args[2]), lens, 1.0)[0]
+    assert (np.abs(_np(out) - want) <= 3.1 * 2.0 ** -8 * size).all()
+    assert (np.abs(_np(lse) - want_lse) <= 2.0 ** -22 * np.abs(want_lse)).all()
