@@ -1,11 +1,12 @@
-"""Attention to a sequence of another length at the ends of its range, in every way the walk over the keys is dealt out: numbers that
-are none, the largest scores."""
+"""Attention to a sequence of another length at the ends of its range, in every way its work is dealt out: numbers that are none, the
+largest scores, samples of enough units to be dealt one after the other."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import block_oracle as bo
 from paper_2512_16093_amd import binding as sla
+from test_gpu_xattn import U, _bounds, _make, _order, _padded_with
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +93,32 @@ def test_the_largest_scores(B, H, Hkv, Nq, Nk, lens, least, most):
     size = bo.xattn_fwd(args[0], args[1], np.abs(args[2]), lens, 1.0)[0]
     assert (np.abs(_np(out) - want) <= 3.1 * 2.0 ** -8 * size).all()
     assert (np.abs(_np(lse) - want_lse) <= 2.0 ** -22 * np.abs(want_lse)).all()
+
+
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,lens,order", [   # units per sample: forward, dq, dk and dv (on 256 compute units)
+    (3, 5, 5, 1700, 100, (100, 0, 57), "token"),         # 70, 70 (no eighths), 45
+    (3, 2, 2, 100, 4800, (4800, 0, 2500), "contiguous"), # 44, 50, 76
+    (2, 11, 11, 300, 1500, (1500, 700), "packed"),       # 132, 165 (pieces), 132
+    (2, 13, 13, 40, 300, (9, 300), "token"),             # 65, 65 (pieces behind a sample's last key), 39
+    (3, 6, 3, 3000, 70, (70, 0, 33), "token"),           # 141, 141, 72 (pieces; heads shared)
+    (2, 7, 7, 1300, 400, None, "packed"),                # 77, 77, 112
+])
+def test_samples_of_many_units(B, H, Hkv, Nq, Nk, lens, order):
+    """A sample of 64 units or more is spread over the whole chip by itself, the next one after it: every row of every sample is
+    written, and right.  (Tolerances: test_gpu_xattn.py.)"""
+    q, k, v, dout, dl = _make(B, H, Hkv, Nq, Nk, lens, order)
+    args = [_np(t) for t in (q, k, v, dout)]
+    want, want_lse = bo.xattn_fwd(*args[:3], lens)
+    wants = bo.xattn_bwd(*args, lens)
+    pv, bq, bk, bv = _bounds(*args, want, lens, 128 ** -0.5)
+    nan = float("nan")
+    g = [_order(t, order) for t in (q, _padded_with(k, lens, nan), _padded_with(v, lens, nan), dout)]
+    fresh = lambda t: _order(torch.full(t.shape, nan, dtype=torch.bfloat16), order)
+    out, lse = sla.xattn_fwd(*g[:3], k_lens=dl, want_lse=True, out=fresh(q))
+    assert (np.abs(_np(out) - want) <= 3.1 * U * pv).all()
+    empty = np.isinf(want_lse)
+    assert (_np(lse)[empty] == -np.inf).all()
+    assert (np.abs(_np(lse)[~empty] - want_lse[~empty]) <= 2.0 ** -20 * (1 + 40.0)).all()
+    got = sla.xattn_bwd(*g[:3], out, g[3], lse, k_lens=dl, grads=[fresh(t) for t in (q, k, v)])
+    for name, x, w, bound in zip(("dq", "dk", "dv"), got, wants, (bq, bk, bv)):
+        assert (np.abs(_np(x) - w) <= 4 * U * bound + 1e-30).all(), name
