@@ -100,3 +100,46 @@ def test_rotation_of_the_largest_values(H, norm):
     dx, _, scale = bo.rope_bwd(_np(dy), _np(x), ang, "interleaved", _np(w), norm)
     got = sla.rope_qk_bwd(dy.cuda(), None, p, plan, q=x.cuda(), q_weight=w.cuda(), norm=norm)
     _near(got[0], dx, scale, "dx")
+
+
+@pytest.mark.parametrize("M,K", [(2, 384), (3, 1536), (4, 128), (4, 5120), (4, 8192), (5, 8192), (5, 384), (1, 13824), (4, 16384)])
+@pytest.mark.parametrize("with_res", [False, True])
+def test_few_rows_quantised_for_a_linear_layer(M, K, with_res):
+    """Either side of the rule for few rows; every row has an amplitude of its own, so that another row's factor would show.  A code
+    is off by half a step and what fp32 adds at 127 steps."""
+    r = np.random.default_rng([M, K, 6])
+    amp = np.array([3.0, 0.01, 200.0, 0.5, 17.0])[:M, None]
+    x, res = (torch.from_numpy((a * amp * r.standard_normal((M, K))).astype(np.float32)).bfloat16() for a in (1.0, 0.3))
+    w = (1 + 0.2 * _bf16(r, K)).bfloat16()
+    h = (x.float() + res.float()).bfloat16() if with_res else x
+    into = torch.full((M, K), float("nan"), dtype=torch.bfloat16, device="cuda") if with_res else None
+    ws, got_h = sla.w8a8_norm_quantize_act(x.cuda(), w.cuda(), res.cuda() if with_res else None, h=into)
+    assert torch.equal(got_h.cpu(), h)
+    n = bo.norm_fwd(_np(h), _np(w), 1e-6)
+    codes, scales = (_np(t) for t in sla.w8a8_debug_unpack(ws, False, M, K))
+    want = np.abs(n.reshape(M, K // 128, 128)).max((0, 2)) / 127
+    assert (np.abs(scales[0] - want) <= F32 * want).all()
+    assert (np.abs(codes - n / np.repeat(want, 128)) <= 0.5 + 127 * 2 * F32).all()
+    # and through the layer: the product of these codes
+    wq = sla.w8a8_quantize_weight(_bf16(r, (256, K), K ** -0.5).cuda())
+    y, _ = sla.w8a8_norm_linear_fwd(x.cuda(), w.cuda(), wq, 256, res=res.cuda() if with_res else None)
+    assert torch.equal(y, sla.w8a8_gemm_fwd(ws, wq, M, 256, K))
+
+
+@pytest.mark.parametrize("M", [1, 3, 4, 5])
+def test_one_row_and_few_of_the_norm(M):
+    """Single tokens at a model's widths, forward and backward."""
+    for K in (1536, 5120, 8960):
+        r = np.random.default_rng([M, K, 7])
+        x, res, dy, dh = (_bf16(r, (M, K), a) for a in (3.0, 0.5, 0.01, 0.01))
+        w = (1 + 0.2 * _bf16(r, K)).bfloat16()
+        y, h = sla.norm_rms_fwd(x.cuda(), w.cuda(), res.cuda())
+        assert torch.equal(h.cpu(), (x.float() + res.float()).bfloat16())
+        want = bo.norm_fwd(_np(h), _np(w), 1e-6)
+        _near(y, want, np.abs(want), "y")
+        got = sla.norm_rms_bwd(dy.cuda(), h, w.cuda(), dh.cuda())
+        dx, dw, scale = bo.norm_bwd(_np(dy), _np(h), _np(w), _np(dh), 1e-6)
+        _near(got[0], dx, scale, "dx")
+        h64 = np.abs(_np(h))
+        terms = (np.abs(_np(dy)) * h64 / np.sqrt((h64 ** 2).mean(1, keepdims=True) + 1e-6)).sum(0)
+        assert (np.abs(_np(got[1]) - dw) <= SUMS * terms).all()
