@@ -631,30 +631,48 @@ __global__ void __launch_bounds__(256) xattn_sum_kernel(XattnSum x) {
 }
 
 // ---------------------------------------------------------------------------
-// A walk of `steps` steps by each of `units` workgroups, of which the chip holds `places` at a time: in how many pieces.  A piece
-// shortens the walk and adds its partial results to what is written and read back (bytes_per_piece at 5 TB/s), and splitting at all
-// adds the launch that joins them.  So the time is  us_per_step * steps / S + 4 us + S * bytes_per_piece / 5 TB/s,  least at
-// S = sqrt(steps us_per_step / (us of a piece)); one piece if that is no more.  Measured (us, in a captured graph): 1 row of 12 heads to 512
-// keys in one piece 13.4, in four 8.5; to 2048 in 8 pieces 12.3, in 64 7.8; 256 of 12 to 4096 in 8 pieces 23.3, in 16 26.0; 1024 of 12 to
-// 512 in one 12.6, in two 19.9.
-static XattnDeal deal(long long units, int nw, int tiles, int walk, int step, long long places, double us_per_step, double bytes_per_piece) {
+// A walk of `steps` steps by each of `units` workgroups: in how many pieces.  A piece shortens the walk and adds its partial results
+// to what is written and read back (bytes_per_piece at 5 TB/s), and splitting at all adds the launch that joins them and what a piece
+// starts and ends with.  A step takes the longer the more workgroups share a compute unit.  So with c of them to a unit the time is
+//   us_per_step(c) * steps / S + us_to_split + S * bytes_per_piece / 5 TB/s,   least at S = sqrt(steps us_per_step(c) / (us of a piece)),
+// of what c to a unit leave room for; one piece if no c makes it less.  Measured (us, in a captured graph): 1 row of 12 heads to 512
+// keys in one piece 12.7, in eight 8.9; to 2048 in 8 pieces 13.7, in 32 8.1; 256 of 12 to 4096 in one 74, in 8 25.7, in 16 26.6; 1024 of
+// 12 to 512 in one 13.4, in two 21.8, to 4096 75 / 60.8, in five 46.2; 2048 of 12 to 2048 in one 41.2, in two 51.9, in four 48.8, to 8192
+// 148 / 145 / 126; 4096 of 12 to 4096 113 / 128.  (With one us_per_step for every c, and 4 us to split, the rule took two pieces for
+// 2048 of 12 to 2048, 512 of 40 to 2048, where one takes 41.2 and two 49.0, and 4096 of 12 to 4096.)
+struct XattnCost {
+  int most;                 // workgroups to a compute unit
+  double us_per_step[4];    // with 1 to `most` of them
+  double us_to_split;
+};
+static XattnDeal deal(long long units, int nw, int tiles, int walk, int step, const XattnCost& cost, double bytes_per_piece) {
   const int steps = (walk + step - 1) / step;
-  const double per_piece = bytes_per_piece / 5e6, whole = steps * us_per_step;
-  long long pieces = (long long)std::sqrt(whole / per_piece);
-  pieces = std::min({pieces, places / std::max<long long>(1, units), (long long)(steps + 1) / 2, (long long)XATTN_PIECES});   // (two steps at least)
-  if (pieces < 2 || whole / pieces + 4.0 + pieces * per_piece >= whole) pieces = 1;
+  const long long places = compute_units();
+  const double per_piece = bytes_per_piece / 5e6;
+  long long pieces = 1;
+  double least = steps * cost.us_per_step[std::min<long long>((units + places - 1) / places, cost.most) - 1];
+  for (int c = 1; c <= cost.most; ++c) {
+    const double whole = steps * cost.us_per_step[c - 1];
+    const long long p = std::min({(long long)std::sqrt(whole / per_piece), c * places / units, (long long)(steps + 1) / 2, (long long)XATTN_PIECES});   // (two steps at least)
+    const double us = p < 2 ? least : whole / p + cost.us_to_split + p * per_piece;
+    if (us < least) {
+      least = us;
+      pieces = p;
+    }
+  }
   const int each = (int)((steps + pieces - 1) / pieces);
   return XattnDeal{nw, tiles, (steps + each - 1) / each, each * step};
 }
 XattnDeal xattn_deal_rows(int B, int G, int rows, int Nk, bool fwd) {
   const int nw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4, tiles = (rows + 32 * nw - 1) / (32 * nw), wide = nw == 4;
-  // places: three (forward) or two (dq) workgroups of four wavefronts to a compute unit, or four of fewer
-  return deal((long long)B * G * tiles, nw, tiles, Nk, fwd || !wide ? 32 : 64, (long long)compute_units() * (!wide ? 4 : fwd ? 3 : 2),
-              !wide ? 0.7 : fwd ? 0.5 : 1.6, (double)B * G * rows * 2 * (D + 4) * 4);
+  static constexpr XattnCost few_rows{4, {0.7, 0.7, 0.7, 0.7}, 4.0}, forward{3, {0.58, 0.87, 1.4}, 10.0}, dq{2, {1.6, 1.6}, 4.0};
+  return deal((long long)B * G * tiles, nw, tiles, Nk, fwd || !wide ? 32 : 64, !wide ? few_rows : fwd ? forward : dq,
+              (double)B * G * rows * 2 * (D + 4) * 4);
 }
 XattnDeal xattn_deal_keys(int B, int G, int group, int Nq, int Nk) {
   const int nw = Nk <= 32 ? 1 : Nk <= 64 ? 2 : 4, tiles = (Nk + 32 * nw - 1) / (32 * nw);
-  return deal((long long)B * G * tiles, nw, tiles, group * ((Nq + 63) / 64), 1, (long long)compute_units() * 2, 2.0, (double)B * G * Nk * 4 * D * 4);
+  static constexpr XattnCost dkv{2, {2.0, 2.0}, 4.0};
+  return deal((long long)B * G * tiles, nw, tiles, group * ((Nq + 63) / 64), 1, dkv, (double)B * G * Nk * 4 * D * 4);
 }
 
 void launch_xattn_fwd(const XattnArgs& a, hipStream_t stream) {
