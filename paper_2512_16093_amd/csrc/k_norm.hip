@@ -182,9 +182,10 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) norm_bwd_kernel(const bf16_
 }
 
 // ---------------------------------------------------------------------------
-// The team and the shares of a thread for K features: F(T, CH).  In the forward direction threads are fitted to two shares each (with
-// 256 threads of three for 5120 features, a sixth of them idle, 75600 rows took 529 us, now 518; 6144 160 / 156); the gradient, whose
-// threads hold sums of dw too, takes three of 256 threads there (568 us; with 320 586; 6144 184 / 207), but two of 512 for 8192 (265 / 231).
+// The team and the shares of a thread for K features: F(T, CH).  In the forward direction, from 2056 to 8192 features, threads are fitted
+// to two shares each, in steps of at most a third; beyond, 1024 threads take whatever there is.  With 256 threads of three for 5120
+// features, a sixth of them idle, 75600 rows took 529 us, now 518; 6144 160 / 156.  The gradient, whose threads hold sums of dw too,
+// takes three of 256 threads there (568 us; with 320 586; 6144 184 / 207), but two of 512 for 8192 (265 / 231).
 #define NORM_TEAMS(K, F)                  \
   do {                                    \
     const int n_ = (K) / 8;               \

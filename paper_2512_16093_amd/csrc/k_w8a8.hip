@@ -153,7 +153,8 @@ __global__ void __launch_bounds__(256) w8a8_quantize_kernel(const bf16_t* __rest
   if (t == 0) scales[kb * RB + rb] = s;
   // codes = the correctly rounded quotient 127 x / amax, rounded to the nearest integer with ties to even
   // (int8_code_word_exact: exact ties stay ties -- with 16-bit inputs they are common, x = amax / 2 is one);
-  // the two's-complement low byte of the returned word is the code; |x / s| <= 127.
+  // the two's-complement low byte of the returned word is the code; |x / s| <= 127.  (With NORM x is an fp32 number and 127 x itself is
+  // rounded: the quotient is then off by up to 2^-23 of its size, and no tie is common.)
   const CodeScale cs = code_scale(amax, 127.0f);
   const float sgn = (negate_odd && (kb & 1)) ? -1.0f : 1.0f;
   unsigned char* out = (unsigned char*)blk;

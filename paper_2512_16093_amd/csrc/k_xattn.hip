@@ -128,7 +128,7 @@ __device__ __forceinline__ float bf16_pair_sum(uint32_t w, float s) {
 // A step is 32 keys: 8 KiB each of K and V in one half of a ring of two.  Kept to 168 registers and 32 KiB, so that three wavefronts
 // share a SIMD: one issues products, one its exponentials, one waits for its queries or for its rows to leave.  With 64 keys a step
 // (224 registers, 64 KiB, two wavefronts): 12 x 32760 queries to 64 keys 39.0 us, now 37.7, to 512 116 / 106, to 8192 1447 / 1405; 40 x
-// 75600 to 512 911 / 842.  For that the operands come in one stream of LDS reads, three ahead of their products (K as rows, then V
+// 75600 to 512 911 / 842 (side by side on one box; 823 to 941 over boxes, by the clock that power leaves them).  For that the operands come in one stream of LDS reads, three ahead of their products (K as rows, then V
 // transposed), the weights are summed on the vector ALU (a product with ones took 16 registers and one in nine of the matrix
 // instructions), and whole walks take two steps a turn, so that the halves of the ring are constants and the addresses of the reads
 // are formed once; the last steps, where a key may not exist, and pieces of a walk go through a body of their own.
@@ -347,6 +347,8 @@ __global__ void __launch_bounds__(256) xattn_join_kernel(XattnArgs a) {
 // ---------------------------------------------------------------------------
 // dS = P o (dO V^T - delta) with P = 2^(S - lse), dQ = scale dS K: three products of a tile pair, S and dP formed again rather than
 // kept (a matrix of 400 MB at 12 x 32760 x 512).  P and dS are fp32 until dS is rounded to the bf16 operand of the last product.
+// delta takes the forward pass's bf16 out: an error of up to 2^-8 |dout| . |out| in it, which is 1.0e-3 of dQ and dK in norm beside 1.7e-3
+// each for dS as a bf16 operand and for the result's own rounding; a sum of P dP in fp32 would take another walk over the keys.
 // Two wavefronts per SIMD (q, dO and dQ alone are 128 registers); 12 x 32760 queries to 512 keys 182 us (0.85 PFLOP/s, 400 MB), at
 // longer walks 1.2 PFLOP/s: power.  Operands read four products ahead in a fixed order: 181.
 template <int NW, bool SPLIT>
@@ -461,7 +463,8 @@ __global__ void __launch_bounds__(NW * 64, 2) xattn_dq_kernel(XattnArgs a) {
 // dV = P^T dO, dK = scale dS^T Q.  A wavefront owns 32 keys and walks over the query rows of every head of its group, 32 QT rows
 // a step; P and dS are rounded to bf16 as operands, the sums stay in fp32 in registers (and in the workspace, where a walk is split:
 // few key blocks have to fill the chip, and their pieces are added up in a fixed order).  12 x 32760 queries to 512 keys, ten pieces: 205
-// us, 1.0 PFLOP/s, the matrix pipe 48 % busy, power; with one wavefront per SIMD and the compiler's order 348.
+// us, 1.0 PFLOP/s, the matrix pipe 49 % busy at 1.93 GHz: neither it nor power (which leaves 1.5 GHz) binds, but the order of LDS
+// reads, exponentials and products in two wavefronts per SIMD.  With one wavefront per SIMD and the compiler's order 348.
 template <int NW, bool SPLIT>
 __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) xattn_dkv_kernel(XattnArgs a) {
   constexpr int QT = 2, STEP_B = 2 * QT * SWZ_TILE_B + 512, STEP = 32 * QT, DEEP = 2;  // Q, dO, then lse2 and -delta of the rows
@@ -519,7 +522,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) xattn_dkv_kernel(Xat
       const unsigned char* stat = ring + half * STEP_B + 2 * QT * SWZ_TILE_B + 16 * hf;
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        // The tile's 32 products take their operands from one stream of LDS reads, four ahead: Q and dO as rows (S, dP), then
+        // The tile's 32 products take their operands from one stream of LDS reads, two ahead: Q and dO as rows (S, dP), then
         // both transposed (dV, dK in turn).  Held to that order, the sums, the keys' operands and what is in flight fit 256
         // registers: two wavefronts share a SIMD.
         const unsigned char *tq = ring + x * SWZ_TILE_B, *td = ring + (QT + x) * SWZ_TILE_B;
