@@ -9,13 +9,15 @@
  *
  * Query heads may share key heads: head h of H reads head h / (H / Hkv) of Hkv.  A sample without keys
  * gives zeros and lse = -infinity.  What lies in keys and values behind k_lens[b] is not used, whatever it is
- * (NaN and infinities included); a NaN in a query or in a key that is used makes the rows that meet it NaN, in out and in lse.
+ * (NaN and infinities included); a NaN in a query or in a key that is used makes the rows that meet it NaN, in
+ * out and in lse.
  * The products run in bf16 on the matrix cores with fp32 accumulation, softmax and its statistics in
  * fp32; the weights are rounded to bf16 for the product with V, and divided by the sum of the ROUNDED
  * weights; lse is that of the unrounded ones.
- * |scale Q.K| up to 2^24 is inside what the forward pass takes: fp32 does not resolve larger scores to a unit, and
- * from 2^31 / log2(e) on a row can come out NaN or as one without keys.  The backward pass forms its weights anew from lse, which is rounded
- * to fp32: they are off by up to 2^-22 |lse| of their size, within a rounding to bf16 up to |lse| = 2^14.
+ * |scale Q.K| up to 2^24 is inside what the forward pass takes: fp32 does not resolve larger scores to a unit,
+ * and from 2^31 / log2(e) on a row can come out NaN or as one without keys.  The backward pass forms its weights
+ * anew from lse, which is rounded to fp32: they are off by up to 2^-22 |lse| of their size, within a rounding to
+ * bf16 up to |lse| = 2^14.
  *
  * Rules as in sla.h: every tensor pointer is a DEVICE pointer owned by the caller, strides are HOST
  * structs; the library allocates nothing and never synchronises; work is enqueued on `stream`; scratch

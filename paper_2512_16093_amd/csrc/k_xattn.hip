@@ -128,10 +128,11 @@ __device__ __forceinline__ float bf16_pair_sum(uint32_t w, float s) {
 // A step is 32 keys: 8 KiB each of K and V in one half of a ring of two.  Kept to 168 registers and 32 KiB, so that three wavefronts
 // share a SIMD: one issues products, one its exponentials, one waits for its queries or for its rows to leave.  With 64 keys a step
 // (224 registers, 64 KiB, two wavefronts): 12 x 32760 queries to 64 keys 39.0 us, now 37.7, to 512 116 / 106, to 8192 1447 / 1405; 40 x
-// 75600 to 512 911 / 842 (side by side on one box; 823 to 941 over boxes, by the clock that power leaves them).  For that the operands come in one stream of LDS reads, three ahead of their products (K as rows, then V
-// transposed), the weights are summed on the vector ALU (a product with ones took 16 registers and one in nine of the matrix
-// instructions), and whole walks take two steps a turn, so that the halves of the ring are constants and the addresses of the reads
-// are formed once; the last steps, where a key may not exist, and pieces of a walk go through a body of their own.
+// 75600 to 512 911 / 842 (side by side on one card; 823 to 944 over cards, by the clock that power leaves them).
+// For that the operands come in one stream of LDS reads, three ahead of their products (K as rows, then V transposed), the weights
+// are summed on the vector ALU (a product with ones took 16 registers and one in nine of the matrix instructions), and whole walks
+// take two steps a turn, so that the halves of the ring are constants and the addresses of the reads are formed once; the last
+// steps, where a key may not exist, and pieces of a walk go through a body of their own.
 template <int NW, bool LSE, bool SPLIT>
 __global__ void __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) xattn_fwd_kernel(XattnArgs a) {
   constexpr int DEEP = 3, STEP = 32, STEP_B = 2 * SWZ_TILE_B;
@@ -656,7 +657,8 @@ static XattnDeal deal(long long units, int nw, int tiles, int walk, int step, co
   double least = steps * cost.us_per_step[std::min<long long>((units + places - 1) / places, cost.most) - 1];
   for (int c = 1; c <= cost.most; ++c) {
     const double whole = steps * cost.us_per_step[c - 1];
-    const long long p = std::min({(long long)std::sqrt(whole / per_piece), c * places / units, (long long)(steps + 1) / 2, (long long)XATTN_PIECES});   // (two steps at least)
+    const long long p = std::min({(long long)std::sqrt(whole / per_piece), c * places / units, (long long)(steps + 1) / 2 /* two steps at least */,
+                                  (long long)XATTN_PIECES});
     const double us = p < 2 ? least : whole / p + cost.us_to_split + p * per_piece;
     if (us < least) {
       least = us;
