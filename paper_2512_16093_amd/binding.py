@@ -8,6 +8,7 @@ returns an error status, an exception is raised.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 
@@ -36,7 +37,10 @@ W8A8_EXPORTS = ("w8a8_weight_bytes", "w8a8_quantize_weight", "w8a8_workspace_byt
                 "w8a8_norm_quantize_act", "w8a8_norm_linear_fwd")
 ROPE_EXPORTS = ("rope_make_plan", "rope_qk_fwd", "rope_bwd_workspace_bytes", "rope_qk_bwd")
 XATTN_EXPORTS = ("xattn_workspace_bytes", "xattn_fwd", "xattn_bwd_workspace_bytes", "xattn_bwd")
-NORM_EXPORTS = ("norm_rms_fwd", "norm_bwd_workspace_bytes", "norm_rms_bwd")
+NORM_EXPORTS = ("norm_rms_fwd", "norm_bwd_workspace_bytes", "norm_rms_bwd", "norm_layer_fwd", "norm_layer_bwd_workspace_bytes",
+                "norm_layer_bwd")
+MXFP4_EXPORTS = ("mxfp4_bytes", "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_pack", "mxfp4_unpack", "mxfp4_gemm_fwd",
+                 "mxfp4_linear_fwd", "mxfp4_norm_quantize", "mxfp4_norm_linear_fwd")
 BWD_EXPORTS = ("sla_bwd_workspace_bytes", "sla_attention_bwd", "sla_saved_bytes", "sla_attention_fwd_train",
                "sla_attention_bwd_saved", "sla_attention_fwd_train_strided", "sla_attention_bwd_strided")
 N_STAGES = 5
@@ -69,6 +73,17 @@ class RopeBwdStrides(ctypes.Structure):
 class XattnBwdStrides(ctypes.Structure):
     """xattn_bwd_strides of include/xattn.h."""
     _fields_ = [(n, ctypes.POINTER(Strides)) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+
+
+class NormModulation(ctypes.Structure):
+    """norm_modulation of include/norm.h."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("gate", "scale", "shift")] + \
+               [(n, ctypes.c_int64) for n in ("gate_stride", "scale_stride", "shift_stride")] + [("rows", ctypes.c_int32)]
+
+
+class NormLayerGrads(ctypes.Structure):
+    """norm_layer_grads of include/norm.h."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w", "b", "gate", "scale", "shift")]
 
 
 class SLAError(RuntimeError):
@@ -186,6 +201,32 @@ def lib():
         L.norm_bwd_workspace_bytes.argtypes = [c_int] * 2
         L.norm_rms_bwd.restype = c_int
         L.norm_rms_bwd.argtypes = [c_vp] * 6 + [c_int] * 2 + [c_dbl, c_vp, c_sz, c_vp]
+        mp = ctypes.POINTER(NormModulation)
+        L.norm_layer_fwd.restype = c_int
+        L.norm_layer_fwd.argtypes = [c_vp] * 4 + [mp] + [c_vp] * 2 + [c_int] * 2 + [c_dbl, c_vp]
+        L.norm_layer_bwd_workspace_bytes.restype = c_sz
+        L.norm_layer_bwd_workspace_bytes.argtypes = [c_int] * 3
+        L.norm_layer_bwd.restype = c_int
+        L.norm_layer_bwd.argtypes = [c_vp] * 6 + [mp, c_vp, c_vp, ctypes.POINTER(NormLayerGrads), c_int, c_int, c_dbl, c_vp, c_sz, c_vp]
+        # include/mxfp4.h
+        L.mxfp4_bytes.restype = c_sz
+        L.mxfp4_bytes.argtypes = [c_int] * 2
+        L.mxfp4_quantize.restype = c_int
+        L.mxfp4_quantize.argtypes = [c_vp, c_int, c_int, c_vp, c_sz, c_vp]
+        L.mxfp4_dequantize.restype = c_int
+        L.mxfp4_dequantize.argtypes = [c_vp, c_sz, c_int, c_int, c_vp, c_vp]
+        L.mxfp4_pack.restype = c_int
+        L.mxfp4_pack.argtypes = [c_vp, c_vp, c_int, c_int, c_vp, c_sz, c_vp]
+        L.mxfp4_unpack.restype = c_int
+        L.mxfp4_unpack.argtypes = [c_vp, c_sz, c_int, c_int, c_vp, c_vp, c_vp]
+        L.mxfp4_gemm_fwd.restype = c_int
+        L.mxfp4_gemm_fwd.argtypes = [c_vp, c_sz, c_vp, c_sz, c_vp, c_vp] + [c_int] * 3 + [c_vp]
+        L.mxfp4_linear_fwd.restype = c_int
+        L.mxfp4_linear_fwd.argtypes = [c_vp, c_vp, c_sz, c_vp, c_vp] + [c_int] * 3 + [c_vp, c_sz, c_vp]
+        L.mxfp4_norm_quantize.restype = c_int
+        L.mxfp4_norm_quantize.argtypes = [c_vp] * 4 + [mp, c_vp, c_vp, c_sz] + [c_int] * 2 + [c_dbl, c_vp]
+        L.mxfp4_norm_linear_fwd.restype = c_int
+        L.mxfp4_norm_linear_fwd.argtypes = ([c_vp] * 4 + [mp, c_vp, c_vp, c_sz, c_vp, c_vp] + [c_int] * 3 + [c_dbl, c_vp, c_sz, c_vp])
         # include/xattn.h
         for f in (L.xattn_workspace_bytes, L.xattn_bwd_workspace_bytes):
             f.restype = c_sz
@@ -842,6 +883,191 @@ def w8a8_norm_linear_fwd(x, norm_w, wq, N, res=None, eps=1e-6, bias=None, worksp
     _rows_of(out, "out", (M, N))
     _launch("w8a8_norm_linear_fwd", x.device, (norm_w, res, h, wq, bias, out, workspace), _at(x), _at(res), _at(norm_w), _at(h), _at(wq),
             _at(bias), _at(out), M, N, K, eps, _at(workspace), workspace.numel())
+    return out, x if res is None else h
+
+
+LayerGrads = collections.namedtuple("LayerGrads", "dx dres dw dbias dgate dscale dshift")
+
+
+def _modulation(M, K, gate, scale, shift):
+    """(norm_modulation or None, samples) of the samples' vectors, each fp32 [samples, K] with contiguous features."""
+    S = 0
+    for t, what in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
+        if t is None:
+            continue
+        if t.dtype != torch.float32 or not t.is_cuda or t.dim() != 2 or t.shape[1] != K or t.stride(1) != 1:
+            raise ValueError("%s: expected a CUDA float32 tensor [samples, %d] with contiguous features" % (what, K))
+        if t.shape[0] < 1 or M % t.shape[0] or (S and t.shape[0] != S):
+            raise ValueError("gate, scale and shift: one number of samples, of M / samples rows each")
+        S = t.shape[0]
+    if S == 0:
+        return None, 1
+    st = [0 if t is None or S == 1 else t.stride(0) for t in (gate, scale, shift)]    # (of one sample the stride says nothing)
+    return NormModulation(_at(gate), _at(scale), _at(shift), *st, M // S), S
+
+
+def _layer_args(x, w, bias, res, gate, scale, shift, h):
+    """(M, K, h, modulation) of a layer norm's forward direction."""
+    M, K = _rows_of(x, "x")
+    _vector(w, "w", K)
+    _vector(bias, "bias", K)
+    if res is not None:
+        _rows_of(res, "res", (M, K))
+        h = torch.empty_like(x) if h is None else h
+        _rows_of(h, "h", (M, K))
+    elif h is not None or gate is not None:
+        raise ValueError("h is written, and a gate applied, only where there is a res")
+    return M, K, h, _modulation(M, K, gate, scale, shift)[0]
+
+
+def norm_layer_fwd(x, w=None, bias=None, res=None, gate=None, scale=None, shift=None, eps=1e-6, out=None, h=None):
+    """(y, h): h = x + gate o res in bf16 (x itself without res), y = (n o w + bias) o (1 + scale) + shift with n the layer norm
+    of h.  w, bias: bf16 [K]; gate, scale, shift: fp32 [samples, K] in any stride, each sample M / samples consecutive rows."""
+    M, K, h, mod = _layer_args(x, w, bias, res, gate, scale, shift, h)
+    out = torch.empty_like(x) if out is None else out
+    _rows_of(out, "out", (M, K))
+    _launch("norm_layer_fwd", x.device, (w, bias, res, gate, scale, shift, out, h), _at(x), _at(res), _at(w), _at(bias),
+            _by_ref(mod), _at(h), _at(out), M, K, eps)
+    return out, x if res is None else h
+
+
+def norm_layer_bwd_workspace_bytes(M, K, rows):
+    return lib().norm_layer_bwd_workspace_bytes(M, K, rows)
+
+
+def norm_layer_bwd(dy, h, w=None, bias=None, dh=None, res=None, gate=None, scale=None, shift=None, eps=1e-6, dx=None, dres=None,
+                   want_vectors=True, workspace=None):
+    """LayerGrads of norm_layer_fwd, h being the stored stream; dh: the gradient that h has from elsewhere.  There is a gradient of
+    each of w, bias, gate (with res), scale and shift that is given, in fp32 (of the last three per sample), unless want_vectors
+    is False; dres is None without a gate: it is dx then."""
+    M, K = _rows_of(dy, "dy")
+    _rows_of(h, "h", (M, K))
+    _vector(w, "w", K)
+    _vector(bias, "bias", K)
+    for t, what in ((dh, "dh"), (res, "res")):
+        if t is not None:
+            _rows_of(t, what, (M, K))
+    mod, S = _modulation(M, K, gate, scale, shift)
+    dx = torch.empty_like(dy) if dx is None else dx
+    _rows_of(dx, "dx", (M, K))
+    if gate is not None:
+        dres = torch.empty_like(dy) if dres is None else dres
+        _rows_of(dres, "dres", (M, K))
+    elif dres is not None:
+        raise ValueError("dres is written only where there is a gate")
+    if want_vectors and gate is not None and res is None:
+        raise ValueError("the gate's gradient needs res")
+    new = lambda t, *shape: torch.empty(shape, dtype=torch.float32, device=dy.device) if want_vectors and t is not None else None
+    dw, db, dgate, dscale, dshift = new(w, K), new(bias, K), new(gate, S, K), new(scale, S, K), new(shift, S, K)
+    grads = None
+    if any(t is not None for t in (dw, db, dgate, dscale, dshift)):
+        grads = NormLayerGrads(_at(dw), _at(db), _at(dgate), _at(dscale), _at(dshift))
+        workspace = _scratch(workspace, norm_layer_bwd_workspace_bytes(M, K, M // S), dy.device, "norm_layer_bwd")
+    _launch("norm_layer_bwd", dy.device, (h, w, bias, dh, res, gate, scale, shift, dx, dres, workspace), _at(dy), _at(dh), _at(h),
+            _at(res), _at(w), _at(bias), _by_ref(mod), _at(dx), _at(dres), _by_ref(grads), M, K, eps, _at(workspace),
+            0 if workspace is None else workspace.numel())
+    return LayerGrads(dx, dres, dw, db, dgate, dscale, dshift)
+
+
+# ---------------------------------------------------------------------------
+# include/mxfp4.h
+# ---------------------------------------------------------------------------
+def mxfp4_bytes(R, K):
+    return lib().mxfp4_bytes(R, K)
+
+
+def _mx_object(q, R, K, what):
+    if q.dtype != torch.uint8 or not q.is_cuda or not q.is_contiguous() or q.numel() < max(1, mxfp4_bytes(R, K)):
+        raise ValueError("%s: expected the object of an [%d, %d] matrix" % (what, R, K))
+
+
+def mxfp4_quantize(x, q=None):
+    """The object (a uint8 tensor) of x bf16 [R, K], weights [N, K] and activations [M, K] alike."""
+    R, K = _rows_of(x, "x")
+    q = _scratch(q, mxfp4_bytes(R, K), x.device, "mxfp4_quantize")
+    _launch("mxfp4_quantize", x.device, (q,), _at(x), R, K, _at(q), q.numel())
+    return q
+
+
+def mxfp4_dequantize(q, R, K, out=None):
+    """What the codes of an object stand for, bf16 [R, K]."""
+    _mx_object(q, R, K, "q")
+    out = torch.empty((R, K), dtype=torch.bfloat16, device=q.device) if out is None else out
+    _rows_of(out, "out", (R, K))
+    _launch("mxfp4_dequantize", q.device, (out,), _at(q), q.numel(), R, K, _at(out))
+    return out
+
+
+def _bytes_2d(t, what, shape):
+    if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError("%s: expected a contiguous CUDA uint8 tensor of %r" % (what, shape))
+
+
+def mxfp4_pack(codes, exponents, q=None):
+    """The object of plain rows: codes uint8 [R, K / 2] (two features a byte, the first in the low half), exponents uint8
+    [R, ceil(K / 32)]."""
+    R, K = codes.shape[0], 2 * codes.shape[1]
+    _bytes_2d(codes, "codes", (R, K // 2))
+    _bytes_2d(exponents, "exponents", (R, -(-K // 32)))
+    q = _scratch(q, mxfp4_bytes(R, K), codes.device, "mxfp4_pack")
+    _launch("mxfp4_pack", codes.device, (exponents, q), _at(codes), _at(exponents), R, K, _at(q), q.numel())
+    return q
+
+
+def mxfp4_unpack(q, R, K):
+    """(codes, exponents) of an object as mxfp4_pack takes them."""
+    _mx_object(q, R, K, "q")
+    codes = torch.empty((R, K // 2), dtype=torch.uint8, device=q.device)
+    exponents = torch.empty((R, -(-K // 32)), dtype=torch.uint8, device=q.device)
+    _launch("mxfp4_unpack", q.device, (), _at(q), q.numel(), R, K, _at(codes), _at(exponents))
+    return codes, exponents
+
+
+def _mx_out(wq, bias, out, M, N, K, device):
+    """The result's tensor, weight and bias checked."""
+    _mx_object(wq, N, K, "wq")
+    _vector(bias, "bias", N)
+    out = torch.empty((M, N), dtype=torch.bfloat16, device=device) if out is None else out
+    _rows_of(out, "out", (M, N))
+    return out
+
+
+def mxfp4_gemm_fwd(xq, wq, M, N, K, bias=None, out=None):
+    """y bf16 [M, N] of the objects of activations [M, K] and a weight [N, K]."""
+    _mx_object(xq, M, K, "xq")
+    out = _mx_out(wq, bias, out, M, N, K, xq.device)
+    _launch("mxfp4_gemm_fwd", xq.device, (wq, bias, out), _at(xq), xq.numel(), _at(wq), wq.numel(), _at(bias), _at(out), M, N, K)
+    return out
+
+
+def mxfp4_linear_fwd(x, wq, N, bias=None, workspace=None, out=None):
+    """y bf16 [M, N] of x bf16 [M, K], quantised on the way, and the object `wq` of an [N, K] weight."""
+    M, K = _rows_of(x, "x")
+    workspace = _scratch(workspace, mxfp4_bytes(M, K), x.device, "mxfp4_linear_fwd")
+    out = _mx_out(wq, bias, out, M, N, K, x.device)
+    _launch("mxfp4_linear_fwd", x.device, (wq, bias, out, workspace), _at(x), _at(wq), wq.numel(), _at(bias), _at(out), M, N, K,
+            _at(workspace), workspace.numel())
+    return out
+
+
+def mxfp4_norm_quantize(x, w=None, bias=None, res=None, gate=None, scale=None, shift=None, eps=1e-6, q=None, h=None):
+    """(q, h): the object of norm_layer_fwd's y, which is not written."""
+    M, K, h, mod = _layer_args(x, w, bias, res, gate, scale, shift, h)
+    q = _scratch(q, mxfp4_bytes(M, K), x.device, "mxfp4_norm_quantize")
+    _launch("mxfp4_norm_quantize", x.device, (w, bias, res, gate, scale, shift, h, q), _at(x), _at(res), _at(w), _at(bias),
+            _by_ref(mod), _at(h), _at(q), q.numel(), M, K, eps)
+    return q, x if res is None else h
+
+
+def mxfp4_norm_linear_fwd(x, wq, N, norm_w=None, norm_bias=None, res=None, gate=None, scale=None, shift=None, eps=1e-6, bias=None,
+                          workspace=None, h=None, out=None):
+    """(y, h): y bf16 [M, N] = the 4-bit layer of norm_layer_fwd's y, with the object `wq` of an [N, K] weight."""
+    M, K, h, mod = _layer_args(x, norm_w, norm_bias, res, gate, scale, shift, h)
+    workspace = _scratch(workspace, mxfp4_bytes(M, K), x.device, "mxfp4_norm_linear_fwd")
+    out = _mx_out(wq, bias, out, M, N, K, x.device)
+    _launch("mxfp4_norm_linear_fwd", x.device, (norm_w, norm_bias, res, gate, scale, shift, h, wq, bias, out, workspace), _at(x),
+            _at(res), _at(norm_w), _at(norm_bias), _by_ref(mod), _at(h), _at(wq), wq.numel(), _at(bias), _at(out), M, N, K, eps,
+            _at(workspace), workspace.numel())
     return out, x if res is None else h
 
 

@@ -1,5 +1,4 @@
-// C ABI of the rotary positions (include/rope.h) and of the root-mean-square norm (include/norm.h): argument checks and
-// the launch sequence.
+// C ABI of the rotary positions (include/rope.h) and of the norms (include/norm.h): argument checks and the launch sequence.
 #pragma GCC visibility push(default)
 #include "../../include/norm.h"
 #include "../../include/rope.h"
@@ -9,6 +8,7 @@
 #include <string.h>
 
 #include "host.h"
+#include "layer.h"
 #include "rows.h"
 
 using namespace sla;
@@ -44,8 +44,6 @@ size_t rope_width(int heads, int norm) { return norm == ROPE_NORM_HEAD ? D : (si
 size_t part_bytes(long long tokens, int heads_max, int heads, int norm) {
   return align256((size_t)rope_bwd_workgroups(tokens, heads_max) * rope_width(heads, norm) * 4);
 }
-bool norm_dims_ok(int M, int K) { return M >= 1 && M <= (1 << 22) && K >= 8 && K <= 16384 && !(K & 7); }
-
 }  // namespace
 
 #pragma GCC visibility push(default)
@@ -177,6 +175,59 @@ int norm_rms_bwd(const void* dy, const void* dh, const void* h, const void* w, v
     if (int st = check_ws(workspace, workspace_bytes, norm_bwd_workspace_bytes(M, K))) return st;
   if (!aligned16(dy) || !aligned16(dh) || !aligned16(h) || !aligned16(w) || !aligned16(dx) || ((uintptr_t)dw & 3)) return SLA_ERR_LAYOUT;
   launch_norm_bwd(dy, dh, h, w, dx, dw, (float*)workspace, M, K, (float)eps, (hipStream_t)stream);
+  return launch_status();
+}
+
+int norm_layer_fwd(const void* x, const void* res, const void* w, const void* b, const norm_modulation* mod, void* h, void* y,
+                   int M, int K, double eps, sla_stream_t stream) {
+  if (!y) return SLA_ERR_NULL;
+  LayerArgs a;
+  if (int st = layer_args(x, res, w, b, mod, h, M, K, eps, &a)) return st;
+  if (!aligned16(y)) return SLA_ERR_LAYOUT;
+  a.y = (bf16_t*)y;
+  launch_layer_fwd(a, (hipStream_t)stream);
+  return launch_status();
+}
+
+size_t norm_layer_bwd_workspace_bytes(int M, int K, int rows) {
+  return norm_dims_ok(M, K) && rows >= 1 ? layer_bwd_bytes(M, K, rows) : 0;
+}
+
+int norm_layer_bwd(const void* dy, const void* dh, const void* h, const void* res, const void* w, const void* b,
+                   const norm_modulation* mod, void* dx, void* dres, const norm_layer_grads* grads, int M, int K, double eps,
+                   void* workspace, size_t workspace_bytes, sla_stream_t stream) {
+  static const norm_layer_grads none = {};
+  const norm_layer_grads& g = grads ? *grads : none;
+  const bool gated = mod && mod->gate;
+  if (!dy || !h || !dx || (dres && !gated) || (g.gate && (!gated || !res))) return SLA_ERR_NULL;
+  if (!norm_dims_ok(M, K) || (mod && mod->rows < 1)) return SLA_ERR_SHAPE;
+  if (!eps_ok(eps)) return SLA_ERR_VALUE;
+  const int rows = mod ? mod->rows : M;
+  if (g.w || g.b || g.gate || g.scale || g.shift)
+    if (int st = check_ws(workspace, workspace_bytes, layer_bwd_bytes(M, K, rows))) return st;
+  const void* const all[] = {dy, dh, h, res, w, b, dx, dres, g.w, g.b, g.gate, g.scale, g.shift};
+  for (const void* p : all)
+    if (!aligned16(p)) return SLA_ERR_LAYOUT;
+  LayerBwdArgs a{};
+  if (mod) {
+    if (int st = sample_vec(mod->gate, mod->gate_stride, &a.gate)) return st;
+    if (int st = sample_vec(mod->scale, mod->scale_stride, &a.scale)) return st;
+  }
+  a.dy = (const bf16_t*)dy;
+  a.dh = (const bf16_t*)dh;
+  a.h = (const bf16_t*)h;
+  a.res = g.gate ? (const bf16_t*)res : nullptr;
+  a.w = (const bf16_t*)w;
+  a.b = (const bf16_t*)b;
+  a.dx = (bf16_t*)dx;
+  a.dres = (bf16_t*)dres;
+  a.grads = g;
+  a.ws = (float*)workspace;
+  a.M = M;
+  a.K = K;
+  a.rows = rows;
+  a.eps = (float)eps;
+  launch_layer_bwd(a, (hipStream_t)stream);
   return launch_status();
 }
 

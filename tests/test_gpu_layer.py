@@ -1,0 +1,215 @@
+"""The layer norm with gate and modulation on the GPU, against the float64 oracle.
+
+Tolerances.  A result in bf16 is off by at most half a step, 2^-8 of its size.  In fp32 before that: a mean over a row is a
+tree of at most 2^-20 of the mean magnitude (chains of up to 32 terms per thread, then pairs, at 2^-24 each), so n is off by
+2^-20 of |n| + r mean|h|, which the oracle's sizes take in place of |n|; factor, vectors and their products add a few 2^-23:
+together below 2^-19 of the terms' sizes forward.  Backward there are two such factors and a mean of their product: 2^-18.  Sums
+over rows: at most 2^-15 of the sum of the terms' sizes for the lengths here (chains of a team's rows, at most a few dozen,
+at 2^-24 each, then short trees; and the terms' own 2^-18)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx_oracle as mo
+from paper_2512_16093_amd import binding as sla
+
+pytestmark = pytest.mark.gpu
+
+HALF, F32, GRAD, SUMS = 2.0 ** -8, 2.0 ** -19, 2.0 ** -18, 2.0 ** -15
+
+
+def _np(t):
+    return None if t is None else t.detach().double().cpu().numpy()
+
+
+def _bf16(r, shape, amp=1.0, add=0.0):
+    return torch.from_numpy((amp * r.standard_normal(shape) + add).astype(np.float32)).bfloat16().cuda()
+
+
+def _six(r, S, K):
+    """A block's six vectors of each sample, as its timestep embedding leaves them."""
+    return torch.from_numpy((0.4 * r.standard_normal((S, 6, K))).astype(np.float32)).cuda()
+
+
+def _near(got, want, size, fp32, what, half=HALF):
+    bad = ~(np.abs(_np(got) - want) <= half * np.abs(want) + fp32 * size + 1e-37)
+    assert not bad.any(), "%s: %d of %d off, worst %.3e" % (what, bad.sum(), bad.size, np.abs(_np(got) - want).max())
+
+
+SHAPES = [  # samples, rows of each, K
+    (1, 1, 8), (1, 1, 128), (3, 1, 520), (1, 129, 1536), (1, 5, 1000), (2, 35, 2048), (3, 11, 2056), (1, 257, 5120), (5, 3, 6136),
+    (2, 3, 8192), (1, 11, 8200), (4, 1, 13824), (1, 3, 16384), (2, 2500, 64), (1, 1300, 4104), (40, 3, 72), (1, 7, 1304), (2, 700, 1528),
+]
+KINDS = ["plain", "affine", "res", "modulated", "gated", "all"]
+
+
+def _inputs(S, rows, K, kind):
+    r = np.random.default_rng([S, rows, K, KINDS.index(kind)])
+    M = S * rows
+    x, res = _bf16(r, (M, K), 2.0, 0.7), _bf16(r, (M, K), 0.8)
+    x[0] = 3.0                                    # a row without deviations: 1 / sqrt(eps) times nothing
+    six = _six(r, S, K)
+    v = {"w": _bf16(r, K, 0.2, 1.0), "bias": _bf16(r, K, 0.3)} if kind in ("affine", "all") else {}
+    if kind in ("modulated", "all"):
+        v.update(scale=six[:, 1], shift=six[:, 0])
+    if kind in ("res", "gated", "all"):
+        v["res"] = res
+    if kind in ("gated", "all"):
+        v["gate"] = six[:, 5]
+    return r, x, v
+
+
+@pytest.mark.parametrize("S,rows,K", SHAPES)
+@pytest.mark.parametrize("kind", KINDS)
+def test_forward_and_backward(S, rows, K, kind):
+    r, x, v = _inputs(S, rows, K, kind)
+    M = S * rows
+    keep = {k: t.clone() for k, t in v.items()}
+    y, h = sla.norm_layer_fwd(x, **v, eps=1e-5)
+    if "res" in v:
+        gate = np.repeat(_np(v["gate"]), rows, 0) if "gate" in v else 1.0
+        step = gate * _np(v["res"])
+        _near(h, _np(x) + step, np.abs(_np(x)) + np.abs(step), 2.0 ** -23, "h")
+    else:
+        assert h is x
+    h64 = _np(h)
+    get = lambda k: _np(v.get(k))
+    want, size = mo.layer_fwd(h64, get("w"), get("bias"), get("scale"), get("shift"), 1e-5)
+    _near(y, want, size, F32, "y")
+    dy, dh = _bf16(r, (M, K), 0.01), _bf16(r, (M, K), 0.01)
+    for up in (None, dh):
+        call = lambda **kw: sla.norm_layer_bwd(dy, h, dh=up, eps=1e-5, **v, **kw)
+        got, again = call(), call()
+        ref = mo.layer_bwd(_np(dy), h64, get("w"), get("bias"), _np(up), get("res"), get("gate"), get("scale"), 1e-5, S)
+        for name in ("dx", "dres"):
+            if getattr(got, name) is not None:
+                _near(getattr(got, name), *ref[name], GRAD, name)
+        for name in ("dw", "dbias", "dgate", "dscale", "dshift"):
+            if getattr(got, name) is not None:
+                _near(getattr(got, name), *ref[name], SUMS, name, half=0.0)
+        given = {"dres": "gate", "dw": "w", "dbias": "bias", "dgate": "gate", "dscale": "scale", "dshift": "shift"}
+        for name, of in given.items():
+            assert (getattr(got, name) is not None) == (of in v), name
+        for a, b in zip(got, again):
+            assert a is None or torch.equal(a, b)
+        bare = call(want_vectors=False)
+        assert torch.equal(bare.dx, got.dx) and all(t is None for t in bare[2:])
+    assert all(torch.equal(v[k], t) for k, t in keep.items())
+
+
+def test_every_vector_by_itself():
+    """Each gradient asked for alone, straight through the C entry point, with nothing else given."""
+    S, rows, K = 3, 50, 712
+    r, x, v = _inputs(S, rows, K, "all")
+    h, dy = sla.norm_layer_fwd(x, **v)[1], _bf16(r, (S * rows, K))
+    every = sla.norm_layer_bwd(dy, h, **v)
+    wanted = {"w": "dw", "b": "dbias", "gate": "dgate", "scale": "dscale", "shift": "dshift"}
+    ws = torch.empty(sla.norm_layer_bwd_workspace_bytes(S * rows, K, rows), dtype=torch.uint8, device="cuda")
+    mod, _ = sla._modulation(S * rows, K, v["gate"], v["scale"], v["shift"])
+    for name, grad in wanted.items():
+        like = getattr(every, grad)
+        out, dx = torch.full_like(like, 7.0), torch.empty_like(dy)
+        g = sla.NormLayerGrads(**{name: out.data_ptr()})
+        sla._launch("norm_layer_bwd", dy.device, (), dy.data_ptr(), None, h.data_ptr(), v["res"].data_ptr(), v["w"].data_ptr(),
+                    v["bias"].data_ptr(), sla._by_ref(mod), dx.data_ptr(), None, sla._by_ref(g), S * rows, K, 1e-6, ws.data_ptr(), ws.numel())
+        assert torch.equal(out, like) and torch.equal(dx, every.dx), name
+    # shift alone, without a scale
+    g = sla.norm_layer_bwd(dy, h, shift=v["shift"])
+    ref = mo.layer_bwd(_np(dy), _np(h), None, None, None, None, None, None, 1e-6, S)
+    _near(g.dshift, *ref["dshift"], SUMS, "dshift", half=0.0)
+    _near(g.dx, *ref["dx"], GRAD, "dx")
+
+
+def test_vectors_in_any_stride_and_one_for_all_samples():
+    S, rows, K = 4, 6, 264
+    r, x, v = _inputs(S, rows, K, "all")
+    same = {k: (t.contiguous() if k in ("gate", "scale", "shift") else t) for k, t in v.items()}
+    assert v["gate"].stride(0) == 6 * K
+    a, b = sla.norm_layer_fwd(x, **v), sla.norm_layer_fwd(x, **same)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))
+    one = {k: (t[:1] if k in ("gate", "scale", "shift") else t) for k, t in v.items()}
+    wide = {k: (t[:1].expand(S, K) if k in ("gate", "scale", "shift") else t) for k, t in v.items()}
+    a, b = sla.norm_layer_fwd(x, **one), sla.norm_layer_fwd(x, **wide)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))
+    dy = _bf16(r, x.shape)
+    ga, gb = sla.norm_layer_bwd(dy, x, **one), sla.norm_layer_bwd(dy, x, **wide)
+    assert torch.equal(ga.dx, gb.dx) and torch.equal(ga.dres, gb.dres)
+    for s, t in zip(ga[4:], gb[4:]):               # of the broadcast vector: the sum over the samples
+        assert torch.allclose(s[0], t.sum(0), rtol=1e-4, atol=1e-5)
+
+
+def test_a_last_sample_that_is_shorter():
+    """Through the C entry points: rows per sample need not divide the number of rows."""
+    M, rows, K = 23, 10, 136
+    r, x, v = _inputs(3, 10, K, "all")
+    mod, _ = sla._modulation(30, K, v["gate"], v["scale"], v["shift"])
+    full = sla.norm_layer_fwd(x, **v)
+    y, h = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    at = lambda t: t.data_ptr()
+    sla._launch("norm_layer_fwd", x.device, (), at(x), at(v["res"]), at(v["w"]), at(v["bias"]), sla._by_ref(mod), at(h), at(y), M, K, 1e-6)
+    assert torch.equal(y[:M], full[0][:M]) and torch.equal(h[:M], full[1][:M]) and (y[M:] == 7).all() and (h[M:] == 7).all()
+    dy = _bf16(r, (30, K))
+    dy[M:] = 0
+    h = full[1]
+    want = sla.norm_layer_bwd(dy, h, **v)          # (no dh: the rows behind the last add nothing to any sum)
+    g = {n: torch.full_like(getattr(want, d), 7.0) for n, d in (("w", "dw"), ("b", "dbias"), ("gate", "dgate"), ("scale", "dscale"), ("shift", "dshift"))}
+    dx, dres = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    need = sla.norm_layer_bwd_workspace_bytes(M, K, rows)
+    ws = torch.full((need + 256,), 9, dtype=torch.uint8, device="cuda")
+    sla._launch("norm_layer_bwd", x.device, (), at(dy), None, at(h), at(v["res"]), at(v["w"]), at(v["bias"]), sla._by_ref(mod), at(dx),
+                at(dres), sla._by_ref(sla.NormLayerGrads(**{n: at(t) for n, t in g.items()})), M, K, 1e-6, at(ws), need)
+    assert torch.equal(dx[:M], want.dx[:M]) and torch.equal(dres[:M], want.dres[:M]) and (dx[M:] == 7).all() and (dres[M:] == 7).all()
+    assert (ws[need:] == 9).all()
+    for n, d in (("w", "dw"), ("b", "dbias"), ("gate", "dgate"), ("scale", "dscale"), ("shift", "dshift")):
+        assert torch.allclose(g[n], getattr(want, d), rtol=1e-4, atol=1e-4), n
+
+
+def test_rows_that_hold_no_number_stay_by_themselves():
+    r = np.random.default_rng(8)
+    x = _bf16(r, (9, 1032), 2.0)
+    x[2, 5], x[4, 1031], x[6, 0] = float("nan"), float("inf"), 3.0e38
+    y = sla.norm_layer_fwd(x)[0]
+    dy = _bf16(r, x.shape)
+    dx = sla.norm_layer_bwd(dy, x, want_vectors=False).dx
+    fine = [0, 1, 3, 5, 7, 8]
+    assert torch.isnan(y[[2, 4]]).all() and torch.isnan(dx[[2, 4]]).all()
+    assert torch.equal(y[fine], sla.norm_layer_fwd(x[fine].contiguous())[0]) and torch.isfinite(y[fine]).all()
+    assert torch.equal(dx[fine], sla.norm_layer_bwd(dy[fine].contiguous(), x[fine].contiguous(), want_vectors=False).dx)
+
+
+def test_a_mean_that_is_large_against_the_deviations():
+    r = np.random.default_rng(9)
+    x = _bf16(r, (5, 4096), 1.0, 200.0)            # (bf16 steps of 1 up there: deviations of a few steps)
+    want, size = mo.layer_fwd(_np(x), None, None, None, None, 1e-6)
+    got = sla.norm_layer_fwd(x)[0]
+    _near(got, want, size, F32, "y")
+    assert np.abs(_np(got) - want).max() < 0.02
+
+
+def test_streams_and_captured_graphs():
+    r, x, v = _inputs(2, 65, 1536, "all")
+    dy, dh = _bf16(r, x.shape), _bf16(r, x.shape)
+
+    def calls():
+        y, h = sla.norm_layer_fwd(x, **v)
+        return [y, h, *sla.norm_layer_bwd(dy, h, dh=dh, **v)]
+    eager = [t.clone() for t in calls()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = calls()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(eager, other))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = calls()
+    for seed in range(3):
+        r = np.random.default_rng([11, seed])
+        for t in (x, dy, dh, v["res"]):
+            t.copy_(_bf16(r, t.shape))
+        v["gate"].copy_(torch.from_numpy(r.standard_normal(v["gate"].shape).astype(np.float32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in held]
+        assert all(torch.equal(a, b) for a, b in zip(replayed, calls())), seed
