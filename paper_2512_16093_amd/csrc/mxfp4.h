@@ -1,9 +1,9 @@
 // The operand order of a matrix in microscaled 4-bit floating point (include/mxfp4.h), and a block's quantisation.
 //
-// A matrix of R rows and K features, RP = R rounded up to 32 and KP = K rounded up to 256, is stored as records of 128 bytes,
-// [KP / 256][RP]: the 256 features of a row, two to a byte (the first in the low half), in eight chunks of 16 bytes, one per
-// block of 32; chunk c of row r stands at position c ^ (r & 7).  Copied to LDS as they are, 32 rows are then read by a
-// wavefront's 64 lanes (32 rows x two chunks) without bank conflicts, and a row's quantised features leave as whole lines.
+// A matrix of R rows and K features, RP = R rounded up to 32 and KP = K rounded up to 256, is stored as records of 64 bytes,
+// [KP / 128][RP]: 128 features of a row, two to a byte (the first in the low half), in four chunks of 16 bytes, one per
+// block of 32; chunk c of row r stands at position c ^ (r / 2 & 3).  Copied to LDS as they are, 32 rows are then read by a
+// wavefront's 64 lanes (32 rows x two chunks) without bank conflicts.
 // The exponents follow, [KP / 256][RP] of 8 bytes: that of block 2 ks + hf at byte 4 hf + ks, so that the word of lane half hf
 // holds what v_mfma_scale_f32_32x32x64_f8f6f4 takes for its four steps ks.  Blocks behind the last feature have codes 0 and
 // the smallest exponent; rows behind the last hold anything (they meet only results that are not stored).
@@ -12,15 +12,16 @@
 
 namespace sla {
 
-constexpr int MX_BLOCK = 32, MX_STEP = 256, MX_REC = MX_STEP / 2;
+constexpr int MX_BLOCK = 32, MX_STEP = 256, MX_REC = 64;
 __host__ __device__ inline int mx_rows(int R) { return (R + 31) / 32 * 32; }
 __host__ __device__ inline int mx_steps(int K) { return (K + MX_STEP - 1) / MX_STEP; }
-inline size_t mx_codes_bytes(int R, int K) { return align256((size_t)mx_rows(R) * mx_steps(K) * MX_REC); }
+inline size_t mx_codes_bytes(int R, int K) { return align256((size_t)mx_rows(R) * mx_steps(K) * (MX_STEP / 2)); }
 inline size_t mx_object_bytes(int R, int K) { return mx_codes_bytes(R, K) + align256((size_t)mx_rows(R) * mx_steps(K) * 8); }
 
-// byte of a block's chunk, and of its exponent
+// byte of the chunk of block c (0..7) of a row's 256 features kb, and of its exponent
+__device__ __forceinline__ int mx_swz(int row) { return (row >> 1) & 3; }
 __device__ __forceinline__ size_t mx_chunk_at(int RP, int row, int kb, int c) {
-  return ((size_t)kb * RP + row) * MX_REC + ((c ^ (row & 7)) << 4);
+  return ((size_t)(2 * kb + (c >> 2)) * RP + row) * MX_REC + (((c & 3) ^ mx_swz(row)) << 4);
 }
 __device__ __forceinline__ size_t mx_exp_at(int RP, int row, int kb, int c) { return ((size_t)kb * RP + row) * 8 + 4 * (c & 1) + (c >> 1); }
 

@@ -119,7 +119,12 @@ GEMM = [  # M, N, K
 ]
 
 
-@pytest.mark.parametrize("M,N,K", GEMM)
+LARGE = [  # one step, two, three and more; few and many token tiles; edges of tokens and outputs
+    (5000, 1800, 200), (4099, 2056, 400), (4099, 2056, 520), (3000, 3080, 1000), (16500, 520, 776), (18000, 456, 256),
+]
+
+
+@pytest.mark.parametrize("M,N,K", GEMM + LARGE)
 def test_linear(M, N, K):
     r = np.random.default_rng([M, N, K])
     x, w, bias = _bf16(r, (M, K), 2.0), _bf16(r, (N, K), K ** -0.5), _bf16(r, N, 0.5).cuda()
@@ -137,7 +142,7 @@ def test_linear(M, N, K):
     _check(sla.mxfp4_gemm_fwd(xq, wq, M, N, K, bias=bias), *_product(xq, wq, M, N, K, bias), K)
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 512, 768), (3, 40, 264), (70, 264, 1032), (600, 1040, 512)])
+@pytest.mark.parametrize("M,N,K", [(1, 512, 768), (3, 40, 264), (70, 264, 1032), (600, 1040, 512), (4100, 2056, 776)])
 def test_rows_and_outputs_that_are_no_numbers_stay_by_themselves(M, N, K):
     """A NaN among the activations makes its row NaN, one in the weight its output; the objects' rows behind the last hold anything."""
     r = np.random.default_rng([M, N, K])
