@@ -2,8 +2,8 @@
 //
 // A matrix of R rows and K features, RP = R rounded up to 32 and KP = K rounded up to 256, is stored as records of 64 bytes,
 // [KP / 128][RP]: 128 features of a row, two to a byte (the first in the low half), in four chunks of 16 bytes, one per
-// block of 32; chunk c of row r stands at position c ^ (r / 2 & 3).  Copied to LDS as they are, 32 rows are then read by a
-// wavefront's 64 lanes (32 rows x two chunks) without bank conflicts.
+// block of 32; chunk c of row r stands at position c ^ (r / 4 & 3).  Copied to LDS as they are, 32 rows are then read by a
+// wavefront's 64 lanes without bank conflicts (16 lanes that read chunk c of 16 rows meet all 64 banks once).
 // The exponents follow, [KP / 256][RP] of 8 bytes: that of block 2 ks + hf at byte 4 hf + ks, so that the word of lane half hf
 // holds what v_mfma_scale_f32_32x32x64_f8f6f4 takes for its four steps ks.  Blocks behind the last feature have codes 0 and
 // the smallest exponent; rows behind the last hold anything (they meet only results that are not stored).
@@ -19,7 +19,7 @@ inline size_t mx_codes_bytes(int R, int K) { return align256((size_t)mx_rows(R) 
 inline size_t mx_object_bytes(int R, int K) { return mx_codes_bytes(R, K) + align256((size_t)mx_rows(R) * mx_steps(K) * 8); }
 
 // byte of the chunk of block c (0..7) of a row's 256 features kb, and of its exponent
-__device__ __forceinline__ int mx_swz(int row) { return (row >> 1) & 3; }
+__device__ __forceinline__ int mx_swz(int row) { return (row >> 2) & 3; }
 __device__ __forceinline__ size_t mx_chunk_at(int RP, int row, int kb, int c) {
   return ((size_t)(2 * kb + (c >> 2)) * RP + row) * MX_REC + (((c & 3) ^ mx_swz(row)) << 4);
 }
