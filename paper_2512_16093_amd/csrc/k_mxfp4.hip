@@ -162,27 +162,42 @@ __global__ void __launch_bounds__(64 * KSPLIT) mxfp4_gemm_split_kernel(const uin
 }
 
 // ---------------------------------------------------------------------------
-// Large calls: workgroup tile 256 tokens x 128 outputs, four wavefronts of 64 x 128, two workgroups per compute unit.  Half a step
-// (128 features: 24 KiB of records) is a stage; three stages are in LDS, copied without registers in between; a step's exponents
-// (3 KiB) ride with its first half, in two places of their own.
+// Large calls: WM x WN wavefronts of RT x CT tiles of 32 tokens x 32 outputs.  Half a step (128 features) is a stage; STAGES of them are
+// in LDS, copied without registers in between; a step's exponents ride with its first half, in two places of their own.
 // A half's first 64 features are read while the second ones of the half before are multiplied; in the middle of a half, when all
-// of its operands are in registers, the workgroup meets: behind that its stage is free for the half three on, and the next half's
+// of its operands are in registers, the workgroup meets: behind that its stage is free for the half STAGES on, and the next half's
 // has arrived.
 // ---------------------------------------------------------------------------
-constexpr int MX_WG_M = 256, MX_WG_N = 128;
-constexpr int MX_STAGE = (MX_WG_M + MX_WG_N) * MX_REC, MX_EXPS = (MX_WG_M + MX_WG_N) * 8;
-constexpr int MX_EPI_STRIDE = MX_WG_N * 2 + 16;   // bytes per staged output row
+constexpr int MX_EPI_PITCH = 16;                  // bytes behind each staged output row
 constexpr int MX_DEAL_MT = 64;                    // token tiles from which whole ones are dealt to the XCDs
 
-__global__ void __launch_bounds__(256, 2) mxfp4_gemm_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ xe,
-                                                            const uint8_t* __restrict__ w, const uint8_t* __restrict__ we,
-                                                            const bf16_t* __restrict__ bias, bf16_t* __restrict__ y, int M, int N,
-                                                            int KB, int MT, int NT) {
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[3 * MX_STAGE + 2 * MX_EXPS];
-  static_assert(4 * 32 * MX_EPI_STRIDE <= 3 * MX_STAGE, "output staging fits the stages");
-  // Workgroups are dealt round-robin over the 8 XCDs.  An XCD walks its tiles in patches of 8 x 8, what its 32 compute units hold
-  // at a time, so that each record of a step is fetched into its L2 once for eight users; of many token tiles it takes every
-  // eighth, of few an eighth of all tiles.
+template <int WM, int WN, int RT, int CT, int STAGES>
+struct MxTile {
+  static constexpr int M = 32 * RT * WM, N = 32 * CT * WN;          // tokens and outputs
+  static constexpr int XP = M / 64, WP = N / 64;                    // a wavefront's pieces (16 records, 1 KiB) of a half
+  static constexpr int EX = M / 128, EW = N / 128;                  // pieces (128 rows, 1 KiB) of a step's exponents: one a wavefront
+  static constexpr int STAGE = (M + N) * MX_REC, EXPS = (M + N) * 8, LDS = STAGES * STAGE + 2 * EXPS;
+  static constexpr int EPI = 32 * CT * 2 + MX_EPI_PITCH;            // bytes of a staged output row
+  // A wavefront's copies of halves `from` .. `to` (counted from a step's first) that are under way where `left` steps follow that one.
+  static constexpr int copies(int from, int to, int left) {
+    int n = 0;
+    for (int h = from; h <= to; ++h) n += h / 2 <= left ? XP + WP + (h % 2 == 0) : 0;
+    return n;
+  }
+  static_assert(WM * WN == 4 && M % 128 == 0 && N % 128 == 0 && EX + EW <= 4 && (STAGES == 3 || STAGES == 4), "the copies' shares");
+  static_assert(4 * 32 * EPI <= STAGES * STAGE && EPI % 16 == 0, "output staging fits the stages");
+};
+
+template <int WM, int WN, int RT, int CT, int STAGES, int PER_CU>
+__global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ xe,
+                                                                 const uint8_t* __restrict__ w, const uint8_t* __restrict__ we,
+                                                                 const bf16_t* __restrict__ bias, bf16_t* __restrict__ y, int M, int N,
+                                                                 int KB, int MT, int NT) {
+  using T = MxTile<WM, WN, RT, CT, STAGES>;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[T::LDS];
+  // Workgroups are dealt round-robin over the 8 XCDs.  An XCD walks its tiles in patches of 8 tiles along the outputs, 4 or 8 along
+  // the tokens, what its 32 compute units hold at a time, so that each record of a step is fetched into its L2 once for several
+  // users; of many token tiles it takes every eighth, of few an eighth of all tiles.
   const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
   const bool deal = MT >= MX_DEAL_MT;
   const int share = (MT * NT + 7) >> 3, first = deal ? 0 : xcd * share, rows = deal ? (MT - xcd + 7) >> 3 : MT;
@@ -194,82 +209,107 @@ __global__ void __launch_bounds__(256, 2) mxfp4_gemm_kernel(const uint8_t* __res
   const int nt = __builtin_amdgcn_readfirstlane(8 * grp + in_grp % cols);
 
   const int t = threadIdx.x, lane = t & 63, wv = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
-  const int RPx = mx_rows(M), RPw = mx_rows(N), H = 2 * KB;
+  const int wm = WN == 1 ? wv : wv / WN, wn = WN == 1 ? 0 : wv % WN;
+  const int RPx = mx_rows(M), RPw = mx_rows(N);
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
 
-  // This wavefront's copies of a half: four pieces (16 records each) of its tokens, two of the weight; of a step's exponents one
-  // (128 rows; the fourth wavefront repeats the third's).  Rows behind the last: the last ones once more.
-  unsigned xo[4], wo[2];
+  // This wavefront's copies: XP pieces of a half's tokens, WP of its weight; one of a step's exponents (wavefronts beyond their
+  // number repeat the last).  Rows behind the last: the last ones once more.
+  unsigned xo[T::XP], wo[T::WP];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) xo[i] = (unsigned)min(mt * MX_WG_M + 64 * wv + 16 * i, RPx - 16) * MX_REC + lane * 16;
+  for (int i = 0; i < T::XP; ++i) xo[i] = (unsigned)min(mt * T::M + 16 * (T::XP * wv + i), RPx - 16) * MX_REC + lane * 16;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) wo[i] = (unsigned)min(nt * MX_WG_N + 32 * wv + 16 * i, RPw - 16) * MX_REC + lane * 16;
-  const bool ex = wv < 2;
-  const unsigned eo = (unsigned)(ex ? min(mt * MX_WG_M + 128 * wv + 2 * lane, RPx - 2) : min(nt * MX_WG_N + 2 * lane, RPw - 2)) * 8;
+  for (int i = 0; i < T::WP; ++i) wo[i] = (unsigned)min(nt * T::N + 16 * (T::WP * wv + i), RPw - 16) * MX_REC + lane * 16;
+  const int ep = min(wv, T::EX + T::EW - 1);
+  const bool ex = ep < T::EX;
+  const unsigned eo = 8u * (unsigned)(ex ? min(mt * T::M + 128 * ep + 2 * lane, RPx - 2) : min(nt * T::N + 128 * (ep - T::EX) + 2 * lane, RPw - 2));
   const char* const e_base = (const char*)(ex ? xe : we);
   const size_t e_step = (size_t)(ex ? RPx : RPw) * 8;
-  auto copy_half = [&](int h, int stage, bool with_exps) __attribute__((always_inline)) {
-    const char *xs = (const char*)x + (size_t)h * RPx * MX_REC, *ws = (const char*)w + (size_t)h * RPw * MX_REC;
-    const unsigned to = lds0 + stage * MX_STAGE;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) copy_piece(xs, xo[i], to + (4 * wv + i) * 1024);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) copy_piece(ws, wo[i], to + MX_WG_M * MX_REC + (2 * wv + i) * 1024);
-    if (with_exps) copy_piece(e_base + (h >> 1) * e_step, eo, lds0 + 3 * MX_STAGE + ((h >> 1) & 1) * MX_EXPS + min(wv, 2) * 1024);
+  // piece i of a half's copies (one more where its step's exponents ride along)
+  auto copy_one = [&](int h, int stage, int i) __attribute__((always_inline)) {
+    const unsigned to = lds0 + stage * T::STAGE;
+    if (i < T::XP) copy_piece((const char*)x + (size_t)h * RPx * MX_REC, xo[i], to + (T::XP * wv + i) * 1024);
+    else if (i < T::XP + T::WP) copy_piece((const char*)w + (size_t)h * RPw * MX_REC, wo[i - T::XP], to + T::M * MX_REC + (T::WP * wv + i - T::XP) * 1024);
+    else copy_piece(e_base + (h >> 1) * e_step, eo, lds0 + STAGES * T::STAGE + ((h >> 1) & 1) * T::EXPS + ep * 1024);
   };
-  // operands: token tiles 2 wv + r, output tiles c
+  auto copy_half = [&](int h, int stage) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < T::XP + T::WP; ++i) copy_one(h, stage, i);
+    if (!(h & 1)) copy_one(h, stage, T::XP + T::WP);
+  };
   const int frag = l32 * MX_REC + ((hf ^ mx_swz(l32)) << 4);
-  auto read_half = [&](int stage, int ks, v4i (&xf)[2], v4i (&wf)[4]) __attribute__((always_inline)) {
-    const unsigned char* s = lds + stage * MX_STAGE + (frag ^ (ks << 5));
-#pragma unroll
-    for (int r = 0; r < 2; ++r) xf[r] = *(const v4i*)(s + (2 * wv + r) * 32 * MX_REC);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) wf[c] = *(const v4i*)(s + MX_WG_M * MX_REC + c * 32 * MX_REC);
+  // operand i of 64 features, in the order the products take them
+  auto read_one = [&](int stage, int ks, int i, v4i (&xf)[RT], v4i (&wf)[CT]) __attribute__((always_inline)) {
+    const unsigned char* s = lds + stage * T::STAGE + (frag ^ (ks << 5));
+    if (i == 0) wf[0] = *(const v4i*)(s + T::M * MX_REC + CT * wn * 32 * MX_REC);
+    else if (i <= RT) xf[i - 1] = *(const v4i*)(s + (RT * wm + i - 1) * 32 * MX_REC);
+    else wf[i - RT] = *(const v4i*)(s + T::M * MX_REC + (CT * wn + i - RT) * 32 * MX_REC);
   };
-  uint32_t xx[2], wx[4];
-  auto read_exps = [&](int step) __attribute__((always_inline)) {
-    const unsigned char* s = lds + 3 * MX_STAGE + (step & 1) * MX_EXPS + 8 * l32 + 4 * hf;
-#pragma unroll
-    for (int r = 0; r < 2; ++r) xx[r] = *(const uint32_t*)(s + (2 * wv + r) * 256);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) wx[c] = *(const uint32_t*)(s + MX_WG_M * 8 + c * 256);
+  auto read_exp = [&](int step, int i, uint32_t (&xs)[RT], uint32_t (&ws)[CT]) __attribute__((always_inline)) {
+    const unsigned char* s = lds + STAGES * T::STAGE + (step & 1) * T::EXPS + 8 * l32 + 4 * hf;
+    if (i < RT) xs[i] = *(const uint32_t*)(s + (RT * wm + i) * 256);
+    else ws[i - RT] = *(const uint32_t*)(s + T::M * 8 + (CT * wn + i - RT) * 256);
   };
-  v16f acc[2][4];
+  v16f acc[RT][CT];
 #pragma unroll
-  for (int r = 0; r < 2; ++r)
+  for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) acc[r][c] = v16f{};
+    for (int c = 0; c < CT; ++c) acc[r][c] = v16f{};
 
-  copy_half(0, 0, true);
-  copy_half(1, 1, false);
-  if (H > 2) {
-    copy_half(2, 2, true);
-    copies_barrier<13>();
+  constexpr int OPS = RT + CT, PIECES = T::XP + T::WP, PRODUCTS = RT * CT;
+  copy_half(0, 0);
+  copy_half(1, 1);
+  if (KB > 1) {
+#pragma unroll
+    for (int h = 2; h < STAGES; ++h) copy_half(h, h);
+    copies_barrier<T::copies(1, STAGES - 1, 1)>();
   } else {
-    copies_barrier<6>();
+    copies_barrier<T::copies(1, 1, 0)>();
   }
-  v4i x0[2], w0[4], x1[2], w1[4];
-  read_half(0, 0, x0, w0);
-  read_exps(0);
+  v4i x0[RT], w0[CT], x1[RT], w1[CT];
+  uint32_t xx[RT], wx[CT], xn[RT], wn_[CT];
+#pragma unroll
+  for (int i = 0; i < OPS; ++i) read_one(0, 0, i, x0, w0);
+#pragma unroll
+  for (int i = 0; i < OPS; ++i) read_exp(0, i, xx, wx);
   int stage = 0;
-#define MX_PRODUCTS(KS, X, W)                                                                    \
-  _Pragma("unroll") for (int c = 0; c < 4; ++c)                                                  \
-  _Pragma("unroll") for (int r = 0; r < 2; ++r) acc[r][c] = mfma_mx<KS>(W[c], wx[c], X[r], xx[r], acc[r][c]); \
-  __builtin_amdgcn_sched_barrier(0);
+// The products of 64 features, and behind each what AFTER(i) asks for: a wavefront alone on its SIMD has to keep the matrix pipe
+// busy by itself.
+#define MX_PRODUCTS(KS, X, W, AFTER)                                                                  \
+  _Pragma("unroll") for (int i = 0; i < PRODUCTS; ++i) {                                              \
+    const int c = i / RT, r = i % RT;                                                                 \
+    acc[r][c] = mfma_mx<KS>(W[c], wx[c], X[r], xx[r], acc[r][c]);                                     \
+    (AFTER)(i);                                                                                       \
+    __builtin_amdgcn_sched_barrier(0);                                                                \
+  }
+// thing number i of n dealt over the products: PER behind each, from product FROM on
+#define MX_DEAL(I, FROM, N, WHAT)                                                                     \
+  {                                                                                                   \
+    constexpr int per_ = ((N) + PRODUCTS - (FROM) - 1) / (PRODUCTS - (FROM));                         \
+    _Pragma("unroll") for (int u_ = 0; u_ < per_; ++u_) {                                             \
+      const int n_ = ((I) - (FROM)) * per_ + u_;                                                      \
+      if ((I) >= (FROM) && n_ < (N)) { WHAT; }                                                        \
+    }                                                                                                 \
+  }
 // (LEFT: steps behind this one, 2 for two or more.  A step is free of branches: the compiler would move the products past them.)
-#define MX_HALF(PART, LEFT)                                                                      \
-  {                                                                                              \
-    const int h = 2 * step + PART, next = stage == 2 ? 0 : stage + 1;                            \
-    read_half(stage, 1, x1, w1);                                                                 \
-    __builtin_amdgcn_sched_barrier(0);                                                           \
-    MX_PRODUCTS(2 * PART, x0, w0)                                                                \
-    copies_barrier<LEFT == 0 ? 0 : PART == 0 ? 7 : 6>();                                         \
-    if constexpr (LEFT + PART >= 2 ? LEFT == 2 : LEFT == 1) copy_half(h + 3, stage, PART == 1);  \
-    if constexpr (LEFT > 0 || PART == 0) read_half(next, 0, x0, w0);                             \
-    __builtin_amdgcn_sched_barrier(0);                                                           \
-    MX_PRODUCTS(2 * PART + 1, x1, w1)                                                            \
-    if constexpr (LEFT > 0 && PART == 1) read_exps(step + 1);                                    \
-    stage = next;                                                                                \
+#define MX_HALF(PART, LEFT)                                                                           \
+  {                                                                                                   \
+    constexpr bool COPY = (PART + STAGES) / 2 <= LEFT, NEXT = LEFT > 0 || PART == 0, EXPS = LEFT > 0 && PART == 1; \
+    constexpr int COPIES = COPY ? PIECES + ((PART + STAGES) % 2 == 0) : 0;                            \
+    const int next = stage == STAGES - 1 ? 0 : stage + 1, ahead = 2 * step + PART + STAGES;           \
+    _Pragma("unroll") for (int n_ = 0; n_ < 2; ++n_) read_one(stage, 1, n_, x1, w1);                  \
+    MX_PRODUCTS(2 * PART, x0, w0, [&](int i) { MX_DEAL(i, 0, OPS - 2, read_one(stage, 1, n_ + 2, x1, w1)) });  \
+    copies_barrier<T::copies(PART + 2, PART + STAGES - 1, LEFT)>();                                   \
+    MX_PRODUCTS(2 * PART + 1, x1, w1, [&](int i) {                                                    \
+      if constexpr (NEXT) MX_DEAL(i, 0, OPS, read_one(next, 0, n_, x0, w0))                           \
+      if constexpr (EXPS) MX_DEAL(i, 0, OPS, read_exp(step + 1, n_, xn, wn_))                         \
+      MX_DEAL(i, PRODUCTS / 4, COPIES, copy_one(ahead, stage, n_))                                    \
+    });                                                                                               \
+    if constexpr (EXPS) {                                                                             \
+      _Pragma("unroll") for (int r = 0; r < RT; ++r) xx[r] = xn[r];                                   \
+      _Pragma("unroll") for (int c = 0; c < CT; ++c) wx[c] = wn_[c];                                  \
+    }                                                                                                 \
+    stage = next;                                                                                     \
   }
   int step = 0;
   for (; step + 2 < KB; ++step) {
@@ -284,45 +324,57 @@ __global__ void __launch_bounds__(256, 2) mxfp4_gemm_kernel(const uint8_t* __res
   MX_HALF(0, 0)
   MX_HALF(1, 0)
 #undef MX_HALF
+#undef MX_DEAL
 #undef MX_PRODUCTS
 
-  // Epilogue: bias in, bf16, through LDS so that rows leave as 256 contiguous bytes, past the caches.  (Behind the last meeting
-  // nobody reads the stages for a result.)
-  unsigned char* my = lds + wv * (32 * MX_EPI_STRIDE);
-  const int n0 = nt * MX_WG_N;
-  uint2 bw[4][4];
+  // Epilogue: bias in, bf16, through LDS so that rows leave as whole lines, past the caches.  (Behind the last meeting nobody reads
+  // the stages.)
+  unsigned char* my = lds + wv * (32 * T::EPI);
+  const int n0 = nt * T::N + 32 * CT * wn;
+  uint2 bw[CT][4];
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
+  for (int c = 0; c < CT; ++c)
 #pragma unroll
     for (int g = 0; g < 4; ++g) bw[c][g] = make_uint2(0u, 0u);
   if (bias) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < CT; ++c)
 #pragma unroll
       for (int g = 0; g < 4; ++g) bw[c][g] = *(const uint2*)(bias + min(n0 + 32 * c + 8 * g + 4 * hf, N - 4));
   }
+  constexpr int LANES = 4 * CT, ROWS = 64 / LANES;    // lanes a row of 32 CT outputs, rows an instruction
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
+  for (int r = 0; r < RT; ++r) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < CT; ++c)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const uint2 b4 = bw[c][g];
         const v16f& f = acc[r][c];
-        *(uint2*)(my + l32 * MX_EPI_STRIDE + (32 * c + 8 * g + 4 * hf) * 2) =
+        *(uint2*)(my + l32 * T::EPI + (32 * c + 8 * g + 4 * hf) * 2) =
             make_uint2(pack_bf16x2(f[4 * g] + bf16_lo(b4.x), f[4 * g + 1] + bf16_hi(b4.x)),
                        pack_bf16x2(f[4 * g + 2] + bf16_lo(b4.y), f[4 * g + 3] + bf16_hi(b4.y)));
       }
     __builtin_amdgcn_wave_barrier();     // (a wavefront's LDS operations execute in order: only the compiler has to keep it)
 #pragma unroll
-    for (int it = 0; it < 8; ++it) {
-      const int row = it * 4 + (lane >> 4), part = lane & 15;
-      const int m = mt * MX_WG_M + 64 * wv + 32 * r + row;
-      const v4i v = *(const v4i*)(my + row * MX_EPI_STRIDE + part * 16);
+    for (int it = 0; it < 32 / ROWS; ++it) {
+      const int row = it * ROWS + lane / LANES, part = lane % LANES;
+      const int m = mt * T::M + 32 * (RT * wm + r) + row;
+      const v4i v = *(const v4i*)(my + row * T::EPI + part * 16);
       if (m < M && n0 + 8 * part < N) __builtin_nontemporal_store(v, (v4i*)(y + (size_t)m * N + n0 + part * 8));
     }
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+template <int WM, int WN, int RT, int CT, int STAGES, int PER_CU>
+static void launch_tiles(const uint8_t* x, const uint8_t* xe, const uint8_t* w, const uint8_t* we, const void* bias, void* y, int M,
+                         int N, int K, hipStream_t stream) {
+  using T = MxTile<WM, WN, RT, CT, STAGES>;
+  const int MT = (M + T::M - 1) / T::M, NT = (N + T::N - 1) / T::N;
+  const unsigned grid = (unsigned)(8 * (MT >= MX_DEAL_MT ? (MT + 7) / 8 * NT : (MT * NT + 7) / 8));
+  mxfp4_gemm_kernel<WM, WN, RT, CT, STAGES, PER_CU><<<grid, 256, 0, stream>>>(x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N,
+                                                                              mx_steps(K), MT, NT);
 }
 
 // ---------------------------------------------------------------------------
@@ -343,14 +395,10 @@ void launch_mxfp4_unpack(const uint8_t* codes, const uint8_t* exps, int R, int K
 }
 void launch_mxfp4_gemm(const uint8_t* x, const uint8_t* xe, const uint8_t* w, const uint8_t* we, const void* bias, void* y, int M,
                        int N, int K, hipStream_t stream) {
-  {
-    const int MT = (M + MX_WG_M - 1) / MX_WG_M, NT = (N + MX_WG_N - 1) / MX_WG_N;
-    if (MT * NT >= 256) {
-      const unsigned grid = (unsigned)(8 * (MT >= MX_DEAL_MT ? (MT + 7) / 8 * NT : (MT * NT + 7) / 8));
-      mxfp4_gemm_kernel<<<grid, 256, 0, stream>>>(x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N, mx_steps(K), MT, NT);
-      return;
-    }
-  }
+#ifndef BIG
+#define BIG 2, 2, 4, 4, 4, 1
+#endif
+  if ((long long)((M + 255) / 256) * ((N + 127) / 128) >= 256) return launch_tiles<BIG>(x, xe, w, we, bias, y, M, N, K, stream);
   const int MT = (M + 63) / 64, NT = (N + 63) / 64;
   mxfp4_gemm_split_kernel<2, 2, 4><<<(unsigned)MT * NT, 256, 0, stream>>>(x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N, mx_steps(K), MT, NT);
 }
