@@ -171,6 +171,27 @@ __global__ void __launch_bounds__(64 * KSPLIT) mxfp4_gemm_split_kernel(const uin
 constexpr int MX_EPI_PITCH = 16;                  // bytes behind each staged output row
 constexpr int MX_DEAL_MT = 64;                    // token tiles from which whole ones are dealt to the XCDs
 
+// Workgroups are dealt round-robin over the 8 XCDs.  An XCD walks its tiles in patches of 8 tiles along the outputs, 4 or 8 along
+// the tokens, what its 32 compute units hold at a time, so that each record of a step is fetched into its L2 once for several
+// users; of many token tiles it takes every eighth, of few an eighth of all tiles.
+struct MxTiles {
+  int first, rows, NT, n, xcd;    // n: tiles of this XCD
+  bool deal;
+  __device__ __forceinline__ MxTiles(int xcd_, int MT, int NT_) : NT(NT_), xcd(xcd_), deal(MT >= MX_DEAL_MT) {
+    const int share = (MT * NT + 7) >> 3;
+    first = deal ? 0 : xcd * share;
+    rows = deal ? (MT - xcd + 7) >> 3 : MT;
+    n = deal ? rows * NT : min(share, MT * NT - first);
+  }
+  __device__ __forceinline__ void at(int slot, int& mt, int& nt) const {
+    const int idx = first + slot, band = idx / (8 * NT), in_band = idx - band * 8 * NT, band_rows = min(8, rows - 8 * band);
+    const int grp = in_band / (8 * band_rows), in_grp = in_band - grp * 8 * band_rows;
+    const int cols = min(8, NT - 8 * grp), row = 8 * band + in_grp / cols;
+    mt = __builtin_amdgcn_readfirstlane(deal ? 8 * row + xcd : row);
+    nt = __builtin_amdgcn_readfirstlane(8 * grp + in_grp % cols);
+  }
+};
+
 template <int WM, int WN, int RT, int CT, int STAGES>
 struct MxTile {
   static constexpr int M = 32 * RT * WM, N = 32 * CT * WN;          // tokens and outputs
@@ -195,19 +216,10 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
                                                                  int KB, int MT, int NT) {
   using T = MxTile<WM, WN, RT, CT, STAGES>;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[T::LDS];
-  // Workgroups are dealt round-robin over the 8 XCDs.  An XCD walks its tiles in patches of 8 tiles along the outputs, 4 or 8 along
-  // the tokens, what its 32 compute units hold at a time, so that each record of a step is fetched into its L2 once for several
-  // users; of many token tiles it takes every eighth, of few an eighth of all tiles.
-  const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
-  const bool deal = MT >= MX_DEAL_MT;
-  const int share = (MT * NT + 7) >> 3, first = deal ? 0 : xcd * share, rows = deal ? (MT - xcd + 7) >> 3 : MT;
-  if (slot >= (deal ? rows * NT : min(share, MT * NT - first))) return;
-  const int idx = first + slot, band = idx / (8 * NT), in_band = idx - band * 8 * NT, band_rows = min(8, rows - 8 * band);
-  const int grp = in_band / (8 * band_rows), in_grp = in_band - grp * 8 * band_rows;
-  const int cols = min(8, NT - 8 * grp), trow = 8 * band + in_grp / cols;
-  const int mt = __builtin_amdgcn_readfirstlane(deal ? 8 * trow + xcd : trow);
-  const int nt = __builtin_amdgcn_readfirstlane(8 * grp + in_grp % cols);
-
+  const MxTiles tiles(blockIdx.x & 7, MT, NT);
+  if ((int)(blockIdx.x >> 3) >= tiles.n) return;
+  int mt, nt;
+  tiles.at(blockIdx.x >> 3, mt, nt);
   const int t = threadIdx.x, lane = t & 63, wv = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
   const int wm = WN == 1 ? wv : wv / WN, wn = WN == 1 ? 0 : wv % WN;
   const int RPx = mx_rows(M), RPw = mx_rows(N);
@@ -367,6 +379,175 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
   }
 }
 
+// The largest calls: tiles of 256 x 256, four wavefronts of 128 x 128, one per SIMD, and one workgroup per compute unit that goes
+// from tile to tile.  The operands of a product then come from LDS for sixteen others instead of eight, a byte copied from L2
+// serves 256 x 256 products of its feature, and nothing waits between tiles: the last half steps of one copy the first of the
+// next, whose first operands are read before the results leave.  Power is what bounds this kernel: every byte that does not move
+// is time.  (K of more than one step.)
+using MxBig = MxTile<2, 2, 4, 4, 3>;
+__global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ xe,
+                                                                 const uint8_t* __restrict__ w, const uint8_t* __restrict__ we,
+                                                                 const bf16_t* __restrict__ bias, bf16_t* __restrict__ y, int M, int N,
+                                                                 int KB, int MT, int NT) {
+  using T = MxBig;
+  constexpr int RT = 4, CT = 4, OPS = RT + CT, PIECES = T::XP + T::WP, PRODUCTS = RT * CT, STAGES = 3;
+  constexpr int AT_EXPS = STAGES * T::STAGE, AT_OUT = AT_EXPS + 2 * T::EXPS, AT_BIAS = AT_OUT + 4 * 32 * T::EPI;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[AT_BIAS + 4 * 256];
+  const MxTiles tiles(blockIdx.x & 7, MT, NT);
+  const int walkers = gridDim.x >> 3;
+  int slot = blockIdx.x >> 3;
+  if (slot >= tiles.n) return;
+  const int t = threadIdx.x, lane = t & 63, wv = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
+  const int wm = wv >> 1, wn = wv & 1;
+  const int RPx = mx_rows(M), RPw = mx_rows(N), H = 2 * KB;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
+  int mt, nt, next_mt, next_nt;
+  tiles.at(slot, mt, nt);
+
+  // Piece i of half h of a tile: pieces are 16 records of the tokens or the weight, whose row is clamped as a whole, and one of the
+  // exponents (wavefronts 0, 1: tokens; 2, 3: weight), two rows a lane.
+  const unsigned lane16 = lane * 16;
+  const bool ex = wv < 2;
+  const char* const e_base = (const char*)(ex ? xe : we);
+  const size_t e_step = (size_t)(ex ? RPx : RPw) * 8;
+  const int e_rows = ex ? RPx : RPw;
+  auto copy_one = [&](int h, int m_, int n_, int stage, int eslot, int i) __attribute__((always_inline)) {
+    const unsigned to = lds0 + stage * T::STAGE;
+    if (i < T::XP) {
+      const int p = T::XP * wv + i;
+      copy_piece((const char*)x + ((size_t)h * RPx + min(m_ * T::M + 16 * p, RPx - 16)) * MX_REC, lane16, to + p * 1024);
+    } else if (i < PIECES) {
+      const int p = T::WP * wv + i - T::XP;
+      copy_piece((const char*)w + ((size_t)h * RPw + min(n_ * T::N + 16 * p, RPw - 16)) * MX_REC, lane16, to + T::M * MX_REC + p * 1024);
+    } else {
+      const int row = min((ex ? m_ * T::M : n_ * T::N) + 128 * wn + 2 * lane, e_rows - 2);
+      copy_piece(e_base + (h >> 1) * e_step, 8u * (unsigned)row, lds0 + AT_EXPS + eslot * T::EXPS + wv * 1024);
+    }
+  };
+  const int frag = l32 * MX_REC + ((hf ^ mx_swz(l32)) << 4);
+  auto read_one = [&](int stage, int ks, int i, v4i (&xf)[RT], v4i (&wf)[CT]) __attribute__((always_inline)) {
+    const unsigned char* s = lds + stage * T::STAGE + (frag ^ (ks << 5));
+    if (i == 0) wf[0] = *(const v4i*)(s + T::M * MX_REC + CT * wn * 32 * MX_REC);
+    else if (i <= RT) xf[i - 1] = *(const v4i*)(s + (RT * wm + i - 1) * 32 * MX_REC);
+    else wf[i - RT] = *(const v4i*)(s + T::M * MX_REC + (CT * wn + i - RT) * 32 * MX_REC);
+  };
+  auto read_exp = [&](int eslot, int i, uint32_t (&xs)[RT], uint32_t (&ws)[CT]) __attribute__((always_inline)) {
+    const unsigned char* s = lds + AT_EXPS + eslot * T::EXPS + 8 * l32 + 4 * hf;
+    if (i < RT) xs[i] = *(const uint32_t*)(s + (RT * wm + i) * 256);
+    else ws[i - RT] = *(const uint32_t*)(s + T::M * 8 + (CT * wn + i - RT) * 256);
+  };
+
+#pragma unroll
+  for (int h = 0; h < STAGES; ++h)
+#pragma unroll
+    for (int i = 0; i < PIECES + (h % 2 == 0); ++i) copy_one(h, mt, nt, h, h >> 1, i);
+  *(uint32_t*)(lds + AT_BIAS + wv * 256 + 4 * lane) = 0u;
+  copies_barrier<0>();
+  v4i x0[RT], w0[CT], x1[RT], w1[CT];
+  uint32_t xx[RT], wx[CT], xn[RT], wn_[CT];
+#pragma unroll
+  for (int i = 0; i < OPS; ++i) read_one(0, 0, i, x0, w0);
+#pragma unroll
+  for (int i = 0; i < OPS; ++i) read_exp(0, i, xx, wx);
+  int stage = 0, eslot = 0;
+  v16f acc[RT][CT];
+
+#define MX_PRODUCTS(KS, FIRST, X, W, AFTER)                                                           \
+  _Pragma("unroll") for (int i = 0; i < PRODUCTS; ++i) {                                              \
+    const int c = i / RT, r = i % RT;                                                                 \
+    acc[r][c] = mfma_mx<KS>(W[c], wx[c], X[r], xx[r], FIRST ? v16f{} : acc[r][c]);                    \
+    (AFTER)(i);                                                                                       \
+    __builtin_amdgcn_sched_barrier(0);                                                                \
+  }
+// The third half on: this tile's, or the next one's.  FIRST: the first step of a tile, whose halves have all been waited for
+// before the results of the tile before left (they are under way, and count like copies).
+#define MX_HALF(PART, FIRST)                                                                          \
+  {                                                                                                   \
+    const int next = stage == STAGES - 1 ? 0 : stage + 1, on = 2 * step + PART + STAGES;              \
+    const bool wrap = on >= H;                                                                        \
+    const int ah = wrap ? on - H : on, am = wrap ? next_mt : mt, an = wrap ? next_nt : nt;            \
+    _Pragma("unroll") for (int i = 0; i < 2; ++i) read_one(stage, 1, i, x1, w1);                      \
+    MX_PRODUCTS(2 * PART, FIRST && PART == 0, x0, w0, [&](int i) { if (i + 2 < OPS) read_one(stage, 1, i + 2, x1, w1); })  \
+    copies_barrier<FIRST ? 63 : T::copies(PART + 2, PART + 2, 2)>();                                  \
+    MX_PRODUCTS(2 * PART + 1, false, x1, w1, [&](int i) {                                             \
+      if (i < OPS) read_one(next, 0, i, x0, w0);                                                      \
+      if (PART == 1 && i < OPS) read_exp(eslot ^ 1, i, xn, wn_);                                      \
+      if (i >= 4 && i - 4 < PIECES + PART) copy_one(ah, am, an, stage, eslot, i - 4);                 \
+    })                                                                                                \
+    if constexpr (PART == 1) {                                                                        \
+      _Pragma("unroll") for (int r = 0; r < RT; ++r) xx[r] = xn[r];                                   \
+      _Pragma("unroll") for (int c = 0; c < CT; ++c) wx[c] = wn_[c];                                  \
+      eslot ^= 1;                                                                                     \
+    }                                                                                                 \
+    stage = next;                                                                                     \
+  }
+  while (true) {
+    const int next_slot = slot + walkers;
+    const bool more = next_slot < tiles.n;
+    tiles.at(more ? next_slot : slot, next_mt, next_nt);   // (behind the last tile its first halves once more, for nobody)
+    const int n0 = nt * T::N + 32 * CT * wn;
+    if (bias) copy_floats((const float*)bias, 2u * (unsigned)min(n0 + 2 * lane, N - 2), lds0 + AT_BIAS + wv * 256);
+    int step = 0;
+    MX_HALF(0, true)
+    MX_HALF(1, true)
+    for (step = 1; step < KB; ++step) {
+      MX_HALF(0, false)
+      MX_HALF(1, false)
+    }
+    // Results: bias in, bf16, through LDS of their own so that rows leave as whole lines, past the caches.  The stores go by a buffer
+    // that ends with the last token and drops what lies behind its end: no branch may stand here, or the sums would be moved out of
+    // their registers all at once.
+    int ln = lane;
+    asm volatile("" : "+v"(ln));         // (nothing of this part is worth a register in the loop)
+    const int q32 = ln & 31, qh = ln >> 5, part = ln & 15, row0 = mt * T::M + 32 * RT * wm;
+    unsigned char* my = lds + AT_OUT + wv * (32 * T::EPI);
+    const unsigned left = (unsigned)max(0, min(M - row0, 32 * RT)) * (2u * (unsigned)N);
+    const uint64_t first = (uint64_t)(uintptr_t)(y + (size_t)row0 * N);      // (uniform, which the compiler does not see)
+    const uint64_t base = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(first >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)first);
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, __builtin_amdgcn_readfirstlane((int)left), 0x00020000);
+    const unsigned at = n0 + 8 * part < N ? (unsigned)(ln >> 4) * (2u * (unsigned)N) + 2u * (n0 + 8 * part) : 0x80000000u;
+    uint2 bw[CT][4];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) bw[c][g] = *(const uint2*)(lds + AT_BIAS + wv * 256 + (32 * c + 8 * g + 4 * qh) * 2);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+#pragma unroll
+      for (int c = 0; c < CT; ++c) asm volatile("" : "+a"(acc[r][c]));   // (not earlier than here)
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const uint2 b4 = bw[c][g];
+          const v16f& f = acc[r][c];
+          *(uint2*)(my + q32 * T::EPI + (32 * c + 8 * g + 4 * qh) * 2) =
+              make_uint2(pack_bf16x2(f[4 * g] + bf16_lo(b4.x), f[4 * g + 1] + bf16_hi(b4.x)),
+                         pack_bf16x2(f[4 * g + 2] + bf16_lo(b4.y), f[4 * g + 3] + bf16_hi(b4.y)));
+        }
+      // (the next tile's first halves: waited for before the first result leaves, behind which they could not be told from it)
+      if (r == 0) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      __builtin_amdgcn_wave_barrier();   // (a wavefront's LDS operations execute in order: only the compiler has to keep it)
+      v4i out[8];
+#pragma unroll
+      for (int it = 0; it < 8; ++it) out[it] = *(const v4i*)(my + (it * 4 + (ln >> 4)) * T::EPI + part * 16);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int it = 0; it < 8; ++it)     // (2: past the caches)
+        __builtin_amdgcn_raw_buffer_store_b128(out[it], buffer, at + (unsigned)(32 * r + 4 * it) * (2u * (unsigned)N), 0, 2);
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!more) break;
+    slot = next_slot;
+    mt = next_mt;
+    nt = next_nt;
+  }
+#undef MX_HALF
+#undef MX_PRODUCTS
+}
+
 template <int WM, int WN, int RT, int CT, int STAGES, int PER_CU>
 static void launch_tiles(const uint8_t* x, const uint8_t* xe, const uint8_t* w, const uint8_t* we, const void* bias, void* y, int M,
                          int N, int K, hipStream_t stream) {
@@ -395,10 +576,17 @@ void launch_mxfp4_unpack(const uint8_t* codes, const uint8_t* exps, int R, int K
 }
 void launch_mxfp4_gemm(const uint8_t* x, const uint8_t* xe, const uint8_t* w, const uint8_t* we, const void* bias, void* y, int M,
                        int N, int K, hipStream_t stream) {
-#ifndef BIG
-#define BIG 2, 2, 4, 4, 4, 1
+#ifndef WALK
+#define WALK 1
 #endif
-  if ((long long)((M + 255) / 256) * ((N + 127) / 128) >= 256) return launch_tiles<BIG>(x, xe, w, we, bias, y, M, N, K, stream);
+  if ((long long)((M + 255) / 256) * ((N + 127) / 128) >= 256) {
+    const int MT = (M + 255) / 256, NT = (N + 255) / 256;
+    if (WALK && K > MX_STEP && (long long)MT * NT >= 256) {
+      mxfp4_gemm_walk_kernel<<<256, 256, 0, stream>>>(x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N, mx_steps(K), MT, NT);
+      return;
+    }
+    return launch_tiles<4, 1, 2, 4, 3, 2>(x, xe, w, we, bias, y, M, N, K, stream);
+  }
   const int MT = (M + 63) / 64, NT = (N + 63) / 64;
   mxfp4_gemm_split_kernel<2, 2, 4><<<(unsigned)MT * NT, 256, 0, stream>>>(x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N, mx_steps(K), MT, NT);
 }

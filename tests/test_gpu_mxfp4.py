@@ -121,6 +121,7 @@ GEMM = [  # M, N, K
 
 LARGE = [  # one step, two, three and more; few and many token tiles; edges of tokens and outputs
     (5000, 1800, 200), (4099, 2056, 400), (4099, 2056, 520), (3000, 3080, 1000), (16500, 520, 776), (18000, 456, 256),
+    (4100, 4104, 264), (4100, 4104, 520), (4352, 4096, 1000), (33000, 520, 1280), (16700, 1032, 512), (5000, 8200, 768),
 ]
 
 
