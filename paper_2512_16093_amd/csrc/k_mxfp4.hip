@@ -171,6 +171,16 @@ __global__ void __launch_bounds__(64 * KSPLIT) mxfp4_gemm_split_kernel(const uin
 constexpr int MX_EPI_PITCH = 16;                  // bytes behind each staged output row
 constexpr int MX_DEAL_MT = 64;                    // token tiles from which whole ones are dealt to the XCDs
 
+// Pieces 2 i and 2 i + 1 of several consecutive ones (the immediate offset moves both addresses).
+__device__ __forceinline__ void copy_pair(const char* base, unsigned off, unsigned lds_addr, int i) {
+  if (i == 0)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0\n\tglobal_load_lds_dwordx4 %1, %0 offset:1024"
+                 : : "s"(base), "v"(off), "s"(lds_addr) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0 offset:2048\n\tglobal_load_lds_dwordx4 %1, %0 offset:3072"
+                 : : "s"(base), "v"(off), "s"(lds_addr) : "memory", "m0");
+}
+
 // Workgroups are dealt round-robin over the 8 XCDs.  An XCD walks its tiles in patches of 8 tiles along the outputs, 4 or 8 along
 // the tokens, what its 32 compute units hold at a time, so that each record of a step is fetched into its L2 once for several
 // users; of many token tiles it takes every eighth, of few an eighth of all tiles.
@@ -196,6 +206,7 @@ template <int WM, int WN, int RT, int CT, int STAGES>
 struct MxTile {
   static constexpr int M = 32 * RT * WM, N = 32 * CT * WN;          // tokens and outputs
   static constexpr int XP = M / 64, WP = N / 64;                    // a wavefront's pieces (16 records, 1 KiB) of a half
+  static constexpr int COPIES = (XP + WP) / 2;                      // ... two at a time
   static constexpr int EX = M / 128, EW = N / 128;                  // pieces (128 rows, 1 KiB) of a step's exponents: one a wavefront
   static constexpr int STAGE = (M + N) * MX_REC, EXPS = (M + N) * 8, LDS = STAGES * STAGE + 2 * EXPS;
   static constexpr int EPI = 32 * CT * 2 + MX_EPI_PITCH;            // bytes of a staged output row
@@ -205,7 +216,7 @@ struct MxTile {
     for (int h = from; h <= to; ++h) n += h / 2 <= left ? XP + WP + (h % 2 == 0) : 0;
     return n;
   }
-  static_assert(WM * WN == 4 && M % 128 == 0 && N % 128 == 0 && EX + EW <= 4 && (STAGES == 3 || STAGES == 4), "the copies' shares");
+  static_assert(WM * WN == 4 && M % 128 == 0 && N % 128 == 0 && M <= MX_TILE_ROWS && N <= MX_TILE_ROWS && EX + EW <= 4 && (STAGES == 3 || STAGES == 4), "the copies' shares");
   static_assert(4 * 32 * EPI <= STAGES * STAGE && EPI % 16 == 0, "output staging fits the stages");
 };
 
@@ -226,28 +237,25 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
 
   // This wavefront's copies: XP pieces of a half's tokens, WP of its weight; one of a step's exponents (wavefronts beyond their
-  // number repeat the last).  Rows behind the last: the last ones once more.
-  unsigned xo[T::XP], wo[T::WP];
-#pragma unroll
-  for (int i = 0; i < T::XP; ++i) xo[i] = (unsigned)min(mt * T::M + 16 * (T::XP * wv + i), RPx - 16) * MX_REC + lane * 16;
-#pragma unroll
-  for (int i = 0; i < T::WP; ++i) wo[i] = (unsigned)min(nt * T::N + 16 * (T::WP * wv + i), RPw - 16) * MX_REC + lane * 16;
+  // number repeat the last).  (Rows behind the last: whatever lies there, see mx_object_bytes.)
+  const unsigned lane16 = lane * 16;
   const int ep = min(wv, T::EX + T::EW - 1);
   const bool ex = ep < T::EX;
-  const unsigned eo = 8u * (unsigned)(ex ? min(mt * T::M + 128 * ep + 2 * lane, RPx - 2) : min(nt * T::N + 128 * (ep - T::EX) + 2 * lane, RPw - 2));
-  const char* const e_base = (const char*)(ex ? xe : we);
+  const char* const px = (const char*)x + ((size_t)mt * T::M + 16 * T::XP * wv) * MX_REC;
+  const char* const pw = (const char*)w + ((size_t)nt * T::N + 16 * T::WP * wv) * MX_REC;
+  const char* const pe = ex ? (const char*)xe + ((size_t)mt * T::M + 128 * ep) * 8 : (const char*)we + ((size_t)nt * T::N + 128 * (ep - T::EX)) * 8;
   const size_t e_step = (size_t)(ex ? RPx : RPw) * 8;
-  // piece i of a half's copies (one more where its step's exponents ride along)
+  // copy i of a half's COPIES, two pieces each (one more where its step's exponents ride along)
   auto copy_one = [&](int h, int stage, int i) __attribute__((always_inline)) {
     const unsigned to = lds0 + stage * T::STAGE;
-    if (i < T::XP) copy_piece((const char*)x + (size_t)h * RPx * MX_REC, xo[i], to + (T::XP * wv + i) * 1024);
-    else if (i < T::XP + T::WP) copy_piece((const char*)w + (size_t)h * RPw * MX_REC, wo[i - T::XP], to + T::M * MX_REC + (T::WP * wv + i - T::XP) * 1024);
-    else copy_piece(e_base + (h >> 1) * e_step, eo, lds0 + STAGES * T::STAGE + ((h >> 1) & 1) * T::EXPS + ep * 1024);
+    if (i < T::XP / 2) copy_pair(px + (size_t)h * RPx * MX_REC, lane16, to + T::XP * wv * 1024, i);
+    else if (i < T::COPIES) copy_pair(pw + (size_t)h * RPw * MX_REC, lane16, to + T::M * MX_REC + T::WP * wv * 1024, i - T::XP / 2);
+    else copy_piece(pe + (h >> 1) * e_step, lane16, lds0 + STAGES * T::STAGE + ((h >> 1) & 1) * T::EXPS + ep * 1024);
   };
   auto copy_half = [&](int h, int stage) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < T::XP + T::WP; ++i) copy_one(h, stage, i);
-    if (!(h & 1)) copy_one(h, stage, T::XP + T::WP);
+    for (int i = 0; i < T::COPIES; ++i) copy_one(h, stage, i);
+    if (!(h & 1)) copy_one(h, stage, T::COPIES);
   };
   const int frag = l32 * MX_REC + ((hf ^ mx_swz(l32)) << 4);
   // operand i of 64 features, in the order the products take them
@@ -268,7 +276,7 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
 #pragma unroll
     for (int c = 0; c < CT; ++c) acc[r][c] = v16f{};
 
-  constexpr int OPS = RT + CT, PIECES = T::XP + T::WP, PRODUCTS = RT * CT;
+  constexpr int OPS = RT + CT, PRODUCTS = RT * CT;
   copy_half(0, 0);
   copy_half(1, 1);
   if (KB > 1) {
@@ -307,7 +315,7 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
 #define MX_HALF(PART, LEFT)                                                                           \
   {                                                                                                   \
     constexpr bool COPY = (PART + STAGES) / 2 <= LEFT, NEXT = LEFT > 0 || PART == 0, EXPS = LEFT > 0 && PART == 1; \
-    constexpr int COPIES = COPY ? PIECES + ((PART + STAGES) % 2 == 0) : 0;                            \
+    constexpr int COPIES = COPY ? T::COPIES + ((PART + STAGES) % 2 == 0) : 0;                         \
     const int next = stage == STAGES - 1 ? 0 : stage + 1, ahead = 2 * step + PART + STAGES;           \
     _Pragma("unroll") for (int n_ = 0; n_ < 2; ++n_) read_one(stage, 1, n_, x1, w1);                  \
     MX_PRODUCTS(2 * PART, x0, w0, [&](int i) { MX_DEAL(i, 0, OPS - 2, read_one(stage, 1, n_ + 2, x1, w1)) });  \
@@ -390,7 +398,7 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
                                                                  const bf16_t* __restrict__ bias, bf16_t* __restrict__ y, int M, int N,
                                                                  int KB, int MT, int NT) {
   using T = MxBig;
-  constexpr int RT = 4, CT = 4, OPS = RT + CT, PIECES = T::XP + T::WP, PRODUCTS = RT * CT, STAGES = 3;
+  constexpr int RT = 4, CT = 4, OPS = RT + CT, PRODUCTS = RT * CT, STAGES = 3;
   constexpr int AT_EXPS = STAGES * T::STAGE, AT_OUT = AT_EXPS + 2 * T::EXPS, AT_BIAS = AT_OUT + 4 * 32 * T::EPI;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[AT_BIAS + 4 * 256];
   const MxTiles tiles(blockIdx.x & 7, MT, NT);
@@ -399,30 +407,25 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
   if (slot >= tiles.n) return;
   const int t = threadIdx.x, lane = t & 63, wv = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
   const int wm = wv >> 1, wn = wv & 1;
-  const int RPx = mx_rows(M), RPw = mx_rows(N), H = 2 * KB;
+  const int RPx = mx_rows(M), RPw = mx_rows(N);
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
   int mt, nt, next_mt, next_nt;
   tiles.at(slot, mt, nt);
 
-  // Piece i of half h of a tile: pieces are 16 records of the tokens or the weight, whose row is clamped as a whole, and one of the
-  // exponents (wavefronts 0, 1: tokens; 2, 3: weight), two rows a lane.
+  // This wavefront's copies of a half: four pieces each of its tokens and its weight, two at a time; one of a step's exponents
+  // (wavefronts 0, 1: tokens; 2, 3: weight).  px, pw, pe: where the next half's lie.  (Rows behind the last: whatever lies there.)
   const unsigned lane16 = lane * 16;
   const bool ex = wv < 2;
-  const char* const e_base = (const char*)(ex ? xe : we);
-  const size_t e_step = (size_t)(ex ? RPx : RPw) * 8;
-  const int e_rows = ex ? RPx : RPw;
-  auto copy_one = [&](int h, int m_, int n_, int stage, int eslot, int i) __attribute__((always_inline)) {
-    const unsigned to = lds0 + stage * T::STAGE;
-    if (i < T::XP) {
-      const int p = T::XP * wv + i;
-      copy_piece((const char*)x + ((size_t)h * RPx + min(m_ * T::M + 16 * p, RPx - 16)) * MX_REC, lane16, to + p * 1024);
-    } else if (i < PIECES) {
-      const int p = T::WP * wv + i - T::XP;
-      copy_piece((const char*)w + ((size_t)h * RPw + min(n_ * T::N + 16 * p, RPw - 16)) * MX_REC, lane16, to + T::M * MX_REC + p * 1024);
-    } else {
-      const int row = min((ex ? m_ * T::M : n_ * T::N) + 128 * wn + 2 * lane, e_rows - 2);
-      copy_piece(e_base + (h >> 1) * e_step, 8u * (unsigned)row, lds0 + AT_EXPS + eslot * T::EXPS + wv * 1024);
-    }
+  const size_t x_half = (size_t)RPx * MX_REC, w_half = (size_t)RPw * MX_REC, e_step = (size_t)(ex ? RPx : RPw) * 8;
+  auto x_at = [&](int m_) { return (const char*)x + ((size_t)m_ * T::M + 64 * wv) * MX_REC; };
+  auto w_at = [&](int n_) { return (const char*)w + ((size_t)n_ * T::N + 64 * wv) * MX_REC; };
+  auto e_at = [&](int m_, int n_) { return (ex ? (const char*)xe + (size_t)m_ * T::M * 8 : (const char*)we + (size_t)n_ * T::N * 8) + 1024 * wn; };
+  const char *px = x_at(mt), *pw = w_at(nt), *pe = e_at(mt, nt);
+  auto copy_one = [&](int stage, int eslot, int i) __attribute__((always_inline)) {
+    const unsigned to = lds0 + stage * T::STAGE + wv * 4096;
+    if (i < 2) copy_pair(px, lane16, to, i);
+    else if (i < 4) copy_pair(pw, lane16, to + T::M * MX_REC, i - 2);
+    else copy_piece(pe, lane16, lds0 + AT_EXPS + eslot * T::EXPS + wv * 1024);
   };
   const int frag = l32 * MX_REC + ((hf ^ mx_swz(l32)) << 4);
   auto read_one = [&](int stage, int ks, int i, v4i (&xf)[RT], v4i (&wf)[CT]) __attribute__((always_inline)) {
@@ -438,9 +441,13 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
   };
 
 #pragma unroll
-  for (int h = 0; h < STAGES; ++h)
+  for (int h = 0; h < STAGES; ++h) {
 #pragma unroll
-    for (int i = 0; i < PIECES + (h % 2 == 0); ++i) copy_one(h, mt, nt, h, h >> 1, i);
+    for (int i = 0; i < T::COPIES + (h % 2 == 0); ++i) copy_one(h, h >> 1, i);
+    px += x_half;
+    pw += w_half;
+    if (h % 2 == 0) pe += e_step;
+  }
   *(uint32_t*)(lds + AT_BIAS + wv * 256 + 4 * lane) = 0u;
   copies_barrier<0>();
   v4i x0[RT], w0[CT], x1[RT], w1[CT];
@@ -463,17 +470,22 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
 // before the results of the tile before left (they are under way, and count like copies).
 #define MX_HALF(PART, FIRST)                                                                          \
   {                                                                                                   \
-    const int next = stage == STAGES - 1 ? 0 : stage + 1, on = 2 * step + PART + STAGES;              \
-    const bool wrap = on >= H;                                                                        \
-    const int ah = wrap ? on - H : on, am = wrap ? next_mt : mt, an = wrap ? next_nt : nt;            \
+    const int next = stage == STAGES - 1 ? 0 : stage + 1;                                             \
+    if (PART == 1) {      /* (the half three on is the next tile's first) */                          \
+      const bool turn = step == KB - 2;                                                               \
+      px = turn ? next_px : px; pw = turn ? next_pw : pw; pe = turn ? next_pe : pe;                   \
+    }                                                                                                 \
     _Pragma("unroll") for (int i = 0; i < 2; ++i) read_one(stage, 1, i, x1, w1);                      \
     MX_PRODUCTS(2 * PART, FIRST && PART == 0, x0, w0, [&](int i) { if (i + 2 < OPS) read_one(stage, 1, i + 2, x1, w1); })  \
     copies_barrier<FIRST ? 63 : T::copies(PART + 2, PART + 2, 2)>();                                  \
     MX_PRODUCTS(2 * PART + 1, false, x1, w1, [&](int i) {                                             \
       if (i < OPS) read_one(next, 0, i, x0, w0);                                                      \
       if (PART == 1 && i < OPS) read_exp(eslot ^ 1, i, xn, wn_);                                      \
-      if (i >= 4 && i - 4 < PIECES + PART) copy_one(ah, am, an, stage, eslot, i - 4);                 \
+      if (i >= 3 && i % 2 == 1 && (i - 3) / 2 < T::COPIES + PART) copy_one(stage, eslot, (i - 3) / 2);  \
     })                                                                                                \
+    px += x_half;                                                                                     \
+    pw += w_half;                                                                                     \
+    if (PART == 1) pe += e_step;                                                                      \
     if constexpr (PART == 1) {                                                                        \
       _Pragma("unroll") for (int r = 0; r < RT; ++r) xx[r] = xn[r];                                   \
       _Pragma("unroll") for (int c = 0; c < CT; ++c) wx[c] = wn_[c];                                  \
@@ -485,6 +497,7 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
     const int next_slot = slot + walkers;
     const bool more = next_slot < tiles.n;
     tiles.at(more ? next_slot : slot, next_mt, next_nt);   // (behind the last tile its first halves once more, for nobody)
+    const char *const next_px = x_at(next_mt), *const next_pw = w_at(next_nt), *const next_pe = e_at(next_mt, next_nt);
     const int n0 = nt * T::N + 32 * CT * wn;
     if (bias) copy_floats((const float*)bias, 2u * (unsigned)min(n0 + 2 * lane, N - 2), lds0 + AT_BIAS + wv * 256);
     int step = 0;

@@ -16,7 +16,12 @@ constexpr int MX_BLOCK = 32, MX_STEP = 256, MX_REC = 64;
 __host__ __device__ inline int mx_rows(int R) { return (R + 31) / 32 * 32; }
 __host__ __device__ inline int mx_steps(int K) { return (K + MX_STEP - 1) / MX_STEP; }
 inline size_t mx_codes_bytes(int R, int K) { return align256((size_t)mx_rows(R) * mx_steps(K) * (MX_STEP / 2)); }
-inline size_t mx_object_bytes(int R, int K) { return mx_codes_bytes(R, K) + align256((size_t)mx_rows(R) * mx_steps(K) * 8); }
+// (the product copies whole tiles of up to 256 rows: behind the last row it reads what follows, at most the records of so many
+// rows behind the end)
+constexpr int MX_TILE_ROWS = 256;
+inline size_t mx_object_bytes(int R, int K) {
+  return mx_codes_bytes(R, K) + align256((size_t)mx_rows(R) * mx_steps(K) * 8) + MX_TILE_ROWS * MX_REC;
+}
 
 // byte of the chunk of block c (0..7) of a row's 256 features kb, and of its exponent
 __device__ __forceinline__ int mx_swz(int row) { return (row >> 2) & 3; }

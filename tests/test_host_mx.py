@@ -80,9 +80,10 @@ def test_layer_norm_argument_errors():
 
 
 def test_object_sizes():
-    assert sla.mxfp4_bytes(1, 8) == 32 * 128 + 256 == sla.mxfp4_bytes(32, 256)
-    assert sla.mxfp4_bytes(33, 264) == 64 * 2 * 128 + 64 * 2 * 8
-    assert sla.mxfp4_bytes(1 << 22, 65536) == (1 << 22) * 256 * 136
+    behind = 256 * 64                                   # (what a tile of the product may read behind the last row)
+    assert sla.mxfp4_bytes(1, 8) == 32 * 128 + 256 + behind == sla.mxfp4_bytes(32, 256)
+    assert sla.mxfp4_bytes(33, 264) == 64 * 2 * 128 + 64 * 2 * 8 + behind
+    assert sla.mxfp4_bytes(1 << 22, 65536) == (1 << 22) * 256 * 136 + behind
     for bad in ((0, 64), (-1, 64), ((1 << 22) + 1, 64), (1, 0), (1, 4), (1, 36), (1, 65544)):
         assert sla.mxfp4_bytes(*bad) == 0, bad
 
