@@ -13,6 +13,8 @@ void launch_mxfp4_pack(const uint8_t* from, const uint8_t* from_exps, int R, int
 void launch_mxfp4_unpack(const uint8_t* codes, const uint8_t* exps, int R, int K, uint8_t* to, uint8_t* to_exps, hipStream_t stream);
 void launch_mxfp4_gemm(const uint8_t* x, const uint8_t* xe, const uint8_t* w, const uint8_t* we, const void* bias, void* y, int M,
                        int N, int K, hipStream_t stream);
+bool launch_mxfp4_linear_few(const void* x, const uint8_t* w, const uint8_t* we, const void* bias, void* y, int M, int N, int K,
+                             hipStream_t stream);
 }  // namespace sla
 
 using namespace sla;
@@ -91,6 +93,7 @@ int mxfp4_linear_fwd(const void* x, const void* wq, size_t wq_bytes, const void*
   if (int st = check_object(workspace, workspace_bytes, M, K)) return st;
   if (int st = layer_out(wq, wq_bytes, bias, y, N, K)) return st;
   if (!aligned16(x)) return SLA_ERR_LAYOUT;
+  if (launch_mxfp4_linear_few(x, (const uint8_t*)wq, exps_of(wq, N, K), bias, y, M, N, K, (hipStream_t)stream)) return launch_status();
   uint8_t *codes = (uint8_t*)workspace, *exps = exps_of(workspace, M, K);
   launch_mxfp4_quantize(x, M, K, codes, exps, (hipStream_t)stream);
   launch_mxfp4_gemm(codes, exps, (const uint8_t*)wq, exps_of(wq, N, K), bias, y, M, N, K, (hipStream_t)stream);

@@ -81,16 +81,28 @@ __device__ __forceinline__ v16f mfma_mx(const v4i& w, uint32_t we, const v4i& x,
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, KS, (int)we, KS, (int)xe);
 }
 
-// Workgroup tile (32 RT) tokens x (32 CT) outputs; its KSPLIT wavefronts split the contraction and meet in LDS in a fixed order.
-// Operands go from memory straight to registers.
-template <int RT, int CT, int KSPLIT>
+// Few tokens or few outputs: workgroup tile (32 RT) tokens x (32 CT) outputs, whose KSPLIT wavefronts split the contraction and meet
+// in LDS in a fixed order.  Operands go from memory straight to registers, a step ahead: nothing is shared between the wavefronts,
+// there is no barrier in the loop.
+// QUANT: the tokens come as bf16, so few (MX_FEW features in all) that every workgroup quantises them by itself, into LDS, while its
+// first weights are on their way: one launch instead of two.
+constexpr int MX_FEW = 32768;
+template <int RT, int CT, int KSPLIT, bool QUANT>
 __global__ void __launch_bounds__(64 * KSPLIT) mxfp4_gemm_split_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ xe,
                                                                        const uint8_t* __restrict__ w, const uint8_t* __restrict__ we,
                                                                        const bf16_t* __restrict__ bias, bf16_t* __restrict__ y, int M,
-                                                                       int N, int KB, int MT, int NT) {
+                                                                       int N, int K, int KB, int MT, int NT) {
   constexpr int PITCH = 36;  // floats per staged row of 32 outputs (16-byte rows, skewed banks)
   __shared__ __attribute__((aligned(16))) float part[KSPLIT][32 * RT][PITCH];
-  const int mt = blockIdx.x % MT, nt = blockIdx.x / MT;
+  static_assert(!QUANT || RT == 1, "up to 32 tokens");
+  __shared__ __attribute__((aligned(16))) uint8_t few[QUANT ? MX_FEW / 2 : 16], few_exps[QUANT ? MX_FEW / 32 : 16];
+  // XCD x takes a contiguous eighth of the tiles, along the smaller operand fastest: of the larger one a tile is then fetched into
+  // one L2 only.
+  const int per = (MT * NT + 7) >> 3, idx = __builtin_amdgcn_readfirstlane((int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3));
+  if ((int)(blockIdx.x >> 3) >= per || idx >= MT * NT) return;
+  const bool tokens_fastest = M <= N;
+  const int major = __builtin_amdgcn_readfirstlane(idx / (tokens_fastest ? MT : NT)), minor = idx - major * (tokens_fastest ? MT : NT);
+  const int nt = tokens_fastest ? major : minor, mt = tokens_fastest ? minor : major;
   const int t = threadIdx.x, lane = t & 63, wv = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, hf = lane >> 5;
   const int RPx = mx_rows(M), RPw = mx_rows(N);
   const int kb0 = KB * wv / KSPLIT, kb1 = KB * (wv + 1) / KSPLIT;
@@ -101,32 +113,64 @@ __global__ void __launch_bounds__(64 * KSPLIT) mxfp4_gemm_split_kernel(const uin
     for (int c = 0; c < CT; ++c) acc[r][c] = v16f{};
   // (tiles behind the last row: the last one once more, nothing of it is stored)
   auto row_of = [&](int tile, int RP) { return min(tile, RP / 32 - 1) * 32 + l32; };
-  for (int kb = kb0; kb < kb1; ++kb) {
+  struct Step {
     v4i a[CT][4], b[RT][4];
     uint32_t ae[CT], be[RT];
+  };
+  auto load = [&](int kb, Step& s) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const int row = row_of(nt * CT + c, RPw);
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) a[c][ks] = *(const v4i*)(w + mx_chunk_at(RPw, row, kb, 2 * ks + hf));
-      ae[c] = *(const uint32_t*)(we + mx_exp_at(RPw, row, kb, hf));
+      for (int ks = 0; ks < 4; ++ks) s.a[c][ks] = *(const v4i*)(w + mx_chunk_at(RPw, row, kb, 2 * ks + hf));
+      s.ae[c] = *(const uint32_t*)(we + mx_exp_at(RPw, row, kb, hf));
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      const int row = row_of(mt * RT + r, RPx);
+      if constexpr (!QUANT) {
+        const int row = row_of(mt * RT + r, RPx);
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) b[r][ks] = *(const v4i*)(x + mx_chunk_at(RPx, row, kb, 2 * ks + hf));
-      be[r] = *(const uint32_t*)(xe + mx_exp_at(RPx, row, kb, hf));
+        for (int ks = 0; ks < 4; ++ks) s.b[r][ks] = *(const v4i*)(x + mx_chunk_at(RPx, row, kb, 2 * ks + hf));
+        s.be[r] = *(const uint32_t*)(xe + mx_exp_at(RPx, row, kb, hf));
+      }
+    }
+  };
+  auto products = [&](int kb, Step& s) __attribute__((always_inline)) {
+    if constexpr (QUANT) {               // (lanes behind the last token: the last one once more, for nobody)
+      const int at = min(l32, M - 1) * KB + kb;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) s.b[0][ks] = *(const v4i*)(few + at * (MX_STEP / 2) + (2 * ks + hf) * 16);
+      s.be[0] = *(const uint32_t*)(few_exps + at * 8 + 4 * hf);
     }
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        acc[r][c] = mfma_mx<0>(a[c][0], ae[c], b[r][0], be[r], acc[r][c]);
-        acc[r][c] = mfma_mx<1>(a[c][1], ae[c], b[r][1], be[r], acc[r][c]);
-        acc[r][c] = mfma_mx<2>(a[c][2], ae[c], b[r][2], be[r], acc[r][c]);
-        acc[r][c] = mfma_mx<3>(a[c][3], ae[c], b[r][3], be[r], acc[r][c]);
+        acc[r][c] = mfma_mx<0>(s.a[c][0], s.ae[c], s.b[r][0], s.be[r], acc[r][c]);
+        acc[r][c] = mfma_mx<1>(s.a[c][1], s.ae[c], s.b[r][1], s.be[r], acc[r][c]);
+        acc[r][c] = mfma_mx<2>(s.a[c][2], s.ae[c], s.b[r][2], s.be[r], acc[r][c]);
+        acc[r][c] = mfma_mx<3>(s.a[c][3], s.ae[c], s.b[r][3], s.be[r], acc[r][c]);
       }
+  };
+  Step s0, s1;
+  if (kb0 < kb1) load(kb0, s0);
+  if constexpr (QUANT) {
+    // (KB * 32 is a multiple of the quad that holds a block)
+    for (int i = t; i < M * KB * 32; i += 64 * KSPLIT) {
+      const int row = i / (KB * 32), k8 = i - row * (KB * 32), c = (k8 >> 2) & 7;
+      const uint4 v = k8 < K / 8 ? *(const uint4*)((const bf16_t*)x + (long long)row * K + 8 * k8) : uint4{0u, 0u, 0u, 0u};
+      const uint32_t e = mx_exponent(__uint_as_float(quad_umax(__float_as_uint(mx_amax8(v)))));
+      *(uint32_t*)(few + 4 * i) = mx_codes8(v, e);
+      if ((k8 & 3) == 0) few_exps[(row * KB + (k8 >> 5)) * 8 + 4 * (c & 1) + (c >> 1)] = (uint8_t)e;
+    }
+    __syncthreads();
+  }
+  for (int kb = kb0; kb < kb1; kb += 2) {   // (a step ahead, the last one once more)
+    load(min(kb + 1, kb1 - 1), s1);
+    products(kb, s0);
+    if (kb + 1 == kb1) break;
+    load(min(kb + 2, kb1 - 1), s0);
+    products(kb + 1, s1);
   }
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
@@ -208,7 +252,9 @@ struct MxTile {
   static constexpr int XP = M / 64, WP = N / 64;                    // a wavefront's pieces (16 records, 1 KiB) of a half
   static constexpr int COPIES = (XP + WP) / 2;                      // ... two at a time
   static constexpr int EX = M / 128, EW = N / 128;                  // pieces (128 rows, 1 KiB) of a step's exponents: one a wavefront
-  static constexpr int STAGE = (M + N) * MX_REC, EXPS = (M + N) * 8, LDS = STAGES * STAGE + 2 * EXPS;
+  static constexpr int STAGE = (M + N) * MX_REC, EXPS = (M + N) * 8;
+  static constexpr int SLOTS = STAGES > 4 ? 4 : 2, LDS = STAGES * STAGE + SLOTS * EXPS;   // (exponents of the steps under way)
+  static constexpr int TAIL = (STAGES + 1) / 2;                     // last steps, behind which less than the usual is copied
   static constexpr int EPI = 32 * CT * 2 + MX_EPI_PITCH;            // bytes of a staged output row
   // A wavefront's copies of halves `from` .. `to` (counted from a step's first) that are under way where `left` steps follow that one.
   static constexpr int copies(int from, int to, int left) {
@@ -216,7 +262,7 @@ struct MxTile {
     for (int h = from; h <= to; ++h) n += h / 2 <= left ? XP + WP + (h % 2 == 0) : 0;
     return n;
   }
-  static_assert(WM * WN == 4 && M % 128 == 0 && N % 128 == 0 && M <= MX_TILE_ROWS && N <= MX_TILE_ROWS && EX + EW <= 4 && (STAGES == 3 || STAGES == 4), "the copies' shares");
+  static_assert(WM * WN == 4 && M % 128 == 0 && N % 128 == 0 && M <= MX_TILE_ROWS && N <= MX_TILE_ROWS && EX + EW <= 4 && STAGES >= 3 && STAGES <= 8, "the copies' shares");
   static_assert(4 * 32 * EPI <= STAGES * STAGE && EPI % 16 == 0, "output staging fits the stages");
 };
 
@@ -243,14 +289,15 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
   const bool ex = ep < T::EX;
   const char* const px = (const char*)x + ((size_t)mt * T::M + 16 * T::XP * wv) * MX_REC;
   const char* const pw = (const char*)w + ((size_t)nt * T::N + 16 * T::WP * wv) * MX_REC;
-  const char* const pe = ex ? (const char*)xe + ((size_t)mt * T::M + 128 * ep) * 8 : (const char*)we + ((size_t)nt * T::N + 128 * (ep - T::EX)) * 8;
+  const char* const pe = ex ? (const char*)xe + ((size_t)mt * T::M + 128 * ep) * 8
+                            : (const char*)we + ((size_t)nt * T::N + 128 * (ep - T::EX)) * 8;
   const size_t e_step = (size_t)(ex ? RPx : RPw) * 8;
   // copy i of a half's COPIES, two pieces each (one more where its step's exponents ride along)
   auto copy_one = [&](int h, int stage, int i) __attribute__((always_inline)) {
     const unsigned to = lds0 + stage * T::STAGE;
     if (i < T::XP / 2) copy_pair(px + (size_t)h * RPx * MX_REC, lane16, to + T::XP * wv * 1024, i);
     else if (i < T::COPIES) copy_pair(pw + (size_t)h * RPw * MX_REC, lane16, to + T::M * MX_REC + T::WP * wv * 1024, i - T::XP / 2);
-    else copy_piece(pe + (h >> 1) * e_step, lane16, lds0 + STAGES * T::STAGE + ((h >> 1) & 1) * T::EXPS + ep * 1024);
+    else copy_piece(pe + (h >> 1) * e_step, lane16, lds0 + STAGES * T::STAGE + ((h >> 1) % T::SLOTS) * T::EXPS + ep * 1024);
   };
   auto copy_half = [&](int h, int stage) __attribute__((always_inline)) {
 #pragma unroll
@@ -266,7 +313,7 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
     else wf[i - RT] = *(const v4i*)(s + T::M * MX_REC + (CT * wn + i - RT) * 32 * MX_REC);
   };
   auto read_exp = [&](int step, int i, uint32_t (&xs)[RT], uint32_t (&ws)[CT]) __attribute__((always_inline)) {
-    const unsigned char* s = lds + STAGES * T::STAGE + (step & 1) * T::EXPS + 8 * l32 + 4 * hf;
+    const unsigned char* s = lds + STAGES * T::STAGE + (step % T::SLOTS) * T::EXPS + 8 * l32 + 4 * hf;
     if (i < RT) xs[i] = *(const uint32_t*)(s + (RT * wm + i) * 256);
     else ws[i - RT] = *(const uint32_t*)(s + T::M * 8 + (CT * wn + i - RT) * 256);
   };
@@ -277,15 +324,12 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
     for (int c = 0; c < CT; ++c) acc[r][c] = v16f{};
 
   constexpr int OPS = RT + CT, PRODUCTS = RT * CT;
-  copy_half(0, 0);
-  copy_half(1, 1);
-  if (KB > 1) {
+  // the first halves; those under way behind the first one are few where there are few steps
 #pragma unroll
-    for (int h = 2; h < STAGES; ++h) copy_half(h, h);
-    copies_barrier<T::copies(1, STAGES - 1, 1)>();
-  } else {
-    copies_barrier<T::copies(1, 1, 0)>();
-  }
+  for (int h = 0; h < STAGES; ++h)
+    if (h < 2 || KB > h / 2) copy_half(h, h);
+  if (KB >= T::TAIL) copies_barrier<T::copies(1, STAGES - 1, T::TAIL - 1)>();
+  else copies_barrier<0>();
   v4i x0[RT], w0[CT], x1[RT], w1[CT];
   uint32_t xx[RT], wx[CT], xn[RT], wn_[CT];
 #pragma unroll
@@ -311,7 +355,7 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
       if ((I) >= (FROM) && n_ < (N)) { WHAT; }                                                        \
     }                                                                                                 \
   }
-// (LEFT: steps behind this one, 2 for two or more.  A step is free of branches: the compiler would move the products past them.)
+// (LEFT: steps behind this one, TAIL for so many or more.  A step is free of branches: the compiler would move the products past them.)
 #define MX_HALF(PART, LEFT)                                                                           \
   {                                                                                                   \
     constexpr bool COPY = (PART + STAGES) / 2 <= LEFT, NEXT = LEFT > 0 || PART == 0, EXPS = LEFT > 0 && PART == 1; \
@@ -332,17 +376,23 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
     stage = next;                                                                                     \
   }
   int step = 0;
-  for (; step + 2 < KB; ++step) {
-    MX_HALF(0, 2)
-    MX_HALF(1, 2)
+  for (; step + T::TAIL < KB; ++step) {
+    MX_HALF(0, T::TAIL)
+    MX_HALF(1, T::TAIL)
   }
-  if (KB > 1) {
-    MX_HALF(0, 1)
-    MX_HALF(1, 1)
-    ++step;
+#define MX_LAST(LEFT)                     \
+  if constexpr (LEFT < T::TAIL) {         \
+    if (KB > LEFT) {                      \
+      MX_HALF(0, LEFT)                    \
+      MX_HALF(1, LEFT)                    \
+      ++step;                             \
+    }                                     \
   }
-  MX_HALF(0, 0)
-  MX_HALF(1, 0)
+  MX_LAST(3)
+  MX_LAST(2)
+  MX_LAST(1)
+  MX_LAST(0)
+#undef MX_LAST
 #undef MX_HALF
 #undef MX_DEAL
 #undef MX_PRODUCTS
@@ -567,8 +617,8 @@ static void launch_tiles(const uint8_t* x, const uint8_t* xe, const uint8_t* w, 
   using T = MxTile<WM, WN, RT, CT, STAGES>;
   const int MT = (M + T::M - 1) / T::M, NT = (N + T::N - 1) / T::N;
   const unsigned grid = (unsigned)(8 * (MT >= MX_DEAL_MT ? (MT + 7) / 8 * NT : (MT * NT + 7) / 8));
-  mxfp4_gemm_kernel<WM, WN, RT, CT, STAGES, PER_CU><<<grid, 256, 0, stream>>>(x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N,
-                                                                              mx_steps(K), MT, NT);
+  mxfp4_gemm_kernel<WM, WN, RT, CT, STAGES, PER_CU><<<grid, 256, 0, stream>>>(
+      x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N, mx_steps(K), MT, NT);
 }
 
 // ---------------------------------------------------------------------------
@@ -587,21 +637,50 @@ void launch_mxfp4_pack(const uint8_t* from, const uint8_t* from_exps, int R, int
 void launch_mxfp4_unpack(const uint8_t* codes, const uint8_t* exps, int R, int K, uint8_t* to, uint8_t* to_exps, hipStream_t stream) {
   mxfp4_unpack_kernel<<<2048, 256, 0, stream>>>(codes, exps, R, K, mx_rows(R), to, to_exps);
 }
+template <int RT, int CT, int KSPLIT, bool QUANT = false>
+static void launch_split(const uint8_t* x, const uint8_t* xe, const uint8_t* w, const uint8_t* we, const void* bias, void* y, int M,
+                         int N, int K, hipStream_t stream) {
+  const int MT = (M + 32 * RT - 1) / (32 * RT), NT = (N + 32 * CT - 1) / (32 * CT);
+  mxfp4_gemm_split_kernel<RT, CT, KSPLIT, QUANT><<<8u * (((unsigned)MT * NT + 7) / 8), 64 * KSPLIT, 0, stream>>>(
+      x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N, K, mx_steps(K), MT, NT);
+}
+
+// Which kernel.  Products alone in us, in a captured graph (walk: 256 x 256 walked; wide: 256 x 128, two to a compute unit; square: 128 x
+// 128 with 3 or 4 stages, three or two to a compute unit; split: RT, CT, wavefronts):
+//   walk from 1024 of its tiles and four steps on: 16384 x 5120 -> 5120 (1280) walk 191, wide 200, 20000 x 1536 -> 8960 (2765) 156 / 158; 12000 x
+//   1536 -> 4608 (846) 59.6 / 48.1, 8192 x 5120 -> 5120 (640) 119 / 113, 65536 x 640 -> 1280 (1280) 47.9 / 46.5;
+//   at least 512 wide tiles: 4096 x 5120 -> 5120 (640) wide 54.9, square 57.1, walk 65; 2048 x 5120 -> 5120 (320) 33.2 / 31.8 / 32.4;
+//   square from 64 tiles on: 1024 x 1536 -> 1536 (96) square 6.0, split 6.9; 256 x 5120 -> 5120 (80) 11.9 / 14.1; 300 x 2560 -> 2560 (60) 7.4 /
+//   6.2; 128 x 5120 -> 5120 (40) 11.4 / 8.7; with four stages up to 256 tiles: 512 x 5120 -> 5120 (160) 12.7 against 13.5, 700 x 8960 -> 1536
+//   (72) 18.4 / 20.6, but 1024 x 5120 -> 5120 (320) 22.1 / 20.9;
+//   split: 64 x 5120 -> 5120 2, 2, 4: 8.7, 1, 2, 4: 7.3; 1 x 5120 -> 5120 1, 1, 4: 5.3, 1, 1, 8: 5.1, 16 x 1536 -> 8960 4.0 / 4.1.
 void launch_mxfp4_gemm(const uint8_t* x, const uint8_t* xe, const uint8_t* w, const uint8_t* we, const void* bias, void* y, int M,
                        int N, int K, hipStream_t stream) {
-#ifndef WALK
-#define WALK 1
-#endif
-  if ((long long)((M + 255) / 256) * ((N + 127) / 128) >= 256) {
-    const int MT = (M + 255) / 256, NT = (N + 255) / 256;
-    if (WALK && K > MX_STEP && (long long)MT * NT >= 256) {
-      mxfp4_gemm_walk_kernel<<<256, 256, 0, stream>>>(x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N, mx_steps(K), MT, NT);
-      return;
-    }
-    return launch_tiles<4, 1, 2, 4, 3, 2>(x, xe, w, we, bias, y, M, N, K, stream);
+  auto tiles = [&](int m, int n) { return (long long)((M + m - 1) / m) * ((N + n - 1) / n); };
+  if (K > 3 * MX_STEP && tiles(256, 256) >= 1024) {
+    mxfp4_gemm_walk_kernel<<<256, 256, 0, stream>>>(x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N, mx_steps(K), (M + 255) / 256, (N + 255) / 256);
+    return;
   }
-  const int MT = (M + 63) / 64, NT = (N + 63) / 64;
-  mxfp4_gemm_split_kernel<2, 2, 4><<<(unsigned)MT * NT, 256, 0, stream>>>(x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N, mx_steps(K), MT, NT);
+#define MX_ARGS x, xe, w, we, bias, y, M, N, K, stream
+  if (tiles(256, 128) >= 512) return launch_tiles<4, 1, 2, 4, 3, 2>(MX_ARGS);
+  if (tiles(128, 128) > 256) return launch_tiles<2, 2, 2, 2, 3, 3>(MX_ARGS);
+  if (tiles(128, 128) >= 64) return launch_tiles<2, 2, 2, 2, 4, 2>(MX_ARGS);
+  if (M > 64) return launch_split<2, 2, 4>(MX_ARGS);
+  if (M > 32) return launch_split<1, 2, 4>(MX_ARGS);
+  if (K > 16 * MX_STEP) return launch_split<1, 1, 8>(MX_ARGS);
+  launch_split<1, 1, 4>(MX_ARGS);
+#undef MX_ARGS
+}
+
+// The layer of bf16 tokens where they are so few that every workgroup quantises them by itself; false: not such a call.  In us, in a
+// captured graph, against two launches: 1 x 5120 -> 5120 5.0 / 7.7, 4 x 5120 6.1 / 7.9, 1 x 1536 -> 8960 3.7 / 7.3, 16 x 1536 7.3 / 8.3, 32 x 1000
+// -> 1000 6.1 / 6.1; beyond, 24 x 1536 -> 8960 9.4 / 8.4, 8 x 5120 -> 5120 7.9 / 8.4.
+bool launch_mxfp4_linear_few(const void* x, const uint8_t* w, const uint8_t* we, const void* bias, void* y, int M, int N, int K,
+                             hipStream_t stream) {
+  if (M > 32 || M * mx_steps(K) * MX_STEP > MX_FEW) return false;
+  if (K > 16 * MX_STEP) launch_split<1, 1, 8, true>((const uint8_t*)x, nullptr, w, we, bias, y, M, N, K, stream);
+  else launch_split<1, 1, 4, true>((const uint8_t*)x, nullptr, w, we, bias, y, M, N, K, stream);
+  return true;
 }
 
 }  // namespace sla

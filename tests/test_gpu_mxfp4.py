@@ -119,9 +119,12 @@ GEMM = [  # M, N, K
 ]
 
 
-LARGE = [  # one step, two, three and more; few and many token tiles; edges of tokens and outputs
-    (5000, 1800, 200), (4099, 2056, 400), (4099, 2056, 520), (3000, 3080, 1000), (16500, 520, 776), (18000, 456, 256),
-    (4100, 4104, 264), (4100, 4104, 520), (4352, 4096, 1000), (33000, 520, 1280), (16700, 1032, 512), (5000, 8200, 768),
+LARGE = [  # every kernel of the larger calls: square tiles (4 and 3 stages), wide, walked; one step, two and more; few and many token
+    # tiles; edges of tokens and outputs
+    (1000, 1032, 200), (1000, 1032, 400), (1000, 1032, 520), (1100, 1304, 776), (1100, 1304, 1800),
+    (2100, 2184, 136), (2100, 2184, 264), (3000, 1800, 520), (2300, 2056, 1536),
+    (5000, 4104, 200), (5000, 4104, 400), (33000, 520, 520), (33000, 520, 776),
+    (8200, 8200, 1000), (66000, 776, 1280), (8193, 8192, 1288), (65600, 1032, 1024),
 ]
 
 
