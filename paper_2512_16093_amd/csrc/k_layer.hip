@@ -14,95 +14,158 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
 
-// MX: codes instead of y.
-template <int T, int CH, bool MX, bool NT>
-__global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs a) {
-  __shared__ float red[2][T / 64];
+// MX: codes instead of y.  A team takes ROWS rows of one sample at a time: two share what they read of the vectors, which come from the
+// caches, 12 bytes a feature with a gate, scale and shift.
+template <int T, int CH, int ROWS, bool MX, bool NT>
+__global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs a, int groups, int per_sample) {
+  __shared__ float red[2][ROWS][T / 64];
   constexpr int TEAMS = T == 64 ? 4 : 1;
-  const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, n = a.K / 8;
+  const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = a.K / 8;
+  const int group = TEAMS * blockIdx.x + (T == 64 ? wave : 0);
+  if (group >= groups) return;                 // (T > 64: the whole workgroup)
   const long long K = a.K;
   const float inv = 1.0f / (float)a.K;
-  for (long long m = (long long)TEAMS * blockIdx.x + (T == 64 ? threadIdx.x >> 6 : 0); m < a.M; m += (long long)TEAMS * gridDim.x) {
-    const long long s = (int)m / a.rows;
-    uint4 v[CH], add[CH];
+  const int s = group / per_sample;
+  const long long m = (long long)s * a.rows + (long long)ROWS * (group - s * per_sample);
+  // (a second row that is not there: the first once more, nothing of it is stored)
+  const bool second = ROWS == 2 && m + 1 < a.M && m + 1 < (long long)(s + 1) * a.rows;
+  auto there = [&](int r) { return r == 0 || second; };
+  auto row = [&](int r) { return m + (there(r) ? r : 0); };
+  // sums of one number per row over the team
+  auto sums = [&](float (&x)[ROWS], float (*mem)[T / 64]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      v[c] = add[c] = uint4{0u, 0u, 0u, 0u};
-      if (t + c * T < n) {
-        v[c] = load_from<NT, uint4>(a.x + m * K + 8ll * (t + c * T));
-        if (a.res) add[c] = load_from<NT, uint4>(a.res + m * K + 8ll * (t + c * T));
+    for (int r = 0; r < ROWS; ++r) x[r] = rows_sum(row_sum(x[r]));
+    if constexpr (T > 64) {
+      if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) mem[r][wave] = x[r];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        x[r] = 0.f;
+#pragma unroll
+        for (int i = 0; i < T / 64; ++i) x[r] += mem[r][i];
       }
     }
-    float sum = 0.f;
+  };
+  uint4 v[ROWS][CH], add[ROWS][CH];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r)
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      float x[8];
-      unpack8(v[c], x);
-      if (a.res && t + c * T < n) {
-        float r[8];
-        unpack8(add[c], r);
-        if (a.gate.v) {
-          float g[8];
-          load8(a.gate.v + s * a.gate.stride + 8 * (t + c * T), g);
+      v[r][c] = add[r][c] = uint4{0u, 0u, 0u, 0u};
+      if (t + c * T < n) {
+        v[r][c] = load_from<NT, uint4>(a.x + row(r) * K + 8ll * (t + c * T));
+        if (a.res) add[r][c] = load_from<NT, uint4>(a.res + row(r) * K + 8ll * (t + c * T));
+      }
+    }
+  // The vectors: of a lone wavefront requested before they are needed, behind what is waited for first, the rows and the sums (65520 x 1536
+  // 153 -> 141 us); of a workgroup when they are needed, there it is the registers that count (75600 x 5120 561 -> 541).
+  constexpr bool EARLY = T == 64;
+  float g[CH][8], sc[CH][8], sh[CH][8];
+  uint4 w[CH] = {}, b[CH] = {};
+  auto gate = [&](int c) __attribute__((always_inline)) {
+    if (a.gate.v) load8(a.gate.v + s * a.gate.stride + 8 * min(t + c * T, n - 1), g[c]);
+  };
+  auto vectors = [&](int c) __attribute__((always_inline)) {
+    const int e = min(t + c * T, n - 1);
+    if (a.w) w[c] = *(const uint4*)(a.w + 8 * e);
+    if (a.b) b[c] = *(const uint4*)(a.b + 8 * e);
+    if (a.scale.v) load8(a.scale.v + s * a.scale.stride + 8 * e, sc[c]);
+    if (a.shift.v) load8(a.shift.v + s * a.shift.stride + 8 * e, sh[c]);
+  };
+  if constexpr (EARLY) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(g[i], r[i], x[i]);
+    for (int c = 0; c < CH; ++c) gate(c);
+  }
+  float mean[ROWS] = {}, rs[ROWS] = {};
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int e = t + c * T;
+    if (e >= n) break;
+    if constexpr (!EARLY) gate(c);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      float x[8], u[8];
+      unpack8(v[r][c], x);
+      if (a.res) {
+        unpack8(add[r][c], u);
+        if (a.gate.v) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(g[c][i], u[i], x[i]);
         } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] += r[i];
+          for (int i = 0; i < 8; ++i) x[i] += u[i];
         }
-        v[c] = pack8(x);
-        store_to<NT>(a.h + m * K + 8ll * (t + c * T), v[c]);
-        unpack8(v[c], x);
+        v[r][c] = pack8(x);
+        if (there(r)) store_to<NT>(a.h + row(r) * K + 8ll * e, v[r][c]);
+        unpack8(v[r][c], x);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += x[i];
+      for (int i = 0; i < 8; ++i) mean[r] += x[i];
     }
-    const float mean = team_sum<T>(sum, red[0]) * inv;
-    float ss = 0.f;
+  }
+  if constexpr (EARLY) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      if (t + c * T >= n) break;
+    for (int c = 0; c < CH; ++c) vectors(c);
+  }
+  sums(mean, red[0]);
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) mean[r] *= inv;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    if (t + c * T >= n) break;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
       float x[8];
-      unpack8(v[c], x);
+      unpack8(v[r][c], x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(x[i] - mean, x[i] - mean, ss);
+      for (int i = 0; i < 8; ++i) rs[r] = __builtin_fmaf(x[i] - mean[r], x[i] - mean[r], rs[r]);
     }
-    const float r = __builtin_amdgcn_rsqf(team_sum<T>(ss, red[1]) * inv + a.eps);
+  }
+  sums(rs, red[1]);
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int e = t + c * T;
-      uint4 out = uint4{0u, 0u, 0u, 0u};
-      if (e < n) {
+  for (int r = 0; r < ROWS; ++r) rs[r] = __builtin_amdgcn_rsqf(rs[r] * inv + a.eps);
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int e = t + c * T;
+    uint4 out[ROWS] = {};
+    if (e < n) {
+      if constexpr (!EARLY) vectors(c);
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
         float x[8], u[8];
-        unpack8(v[c], x);
+        unpack8(v[r][c], x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean) * r;
+        for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean[r]) * rs[r];
         if (a.w) {
-          unpack8(*(const uint4*)(a.w + 8 * e), u);
+          unpack8(w[c], u);
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] *= u[i];
         }
         if (a.b) {
-          unpack8(*(const uint4*)(a.b + 8 * e), u);
+          unpack8(b[c], u);
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] += u[i];
         }
         if (a.scale.v) {
-          load8(a.scale.v + s * a.scale.stride + 8 * e, u);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i], u[i], x[i]);
+          for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i], sc[c][i], x[i]);
         }
         if (a.shift.v) {
-          load8(a.shift.v + s * a.shift.stride + 8 * e, u);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] += u[i];
+          for (int i = 0; i < 8; ++i) x[i] += sh[c][i];
         }
-        out = pack8(x);
+        out[r] = pack8(x);
       }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
       if constexpr (MX) {
-        if (e < mx_steps(a.K) * (MX_STEP / 8)) mx_store8(out, (int)m, e, mx_rows(a.M), a.codes, a.exps);
+        if (e < mx_steps(a.K) * (MX_STEP / 8) && there(r)) mx_store8(out[r], (int)row(r), e, mx_rows(a.M), a.codes, a.exps);
       } else {
-        if (e < n) store_to<NT>(a.y + m * K + 8ll * e, out);
+        if (e < n && there(r)) store_to<NT>(a.y + row(r) * K + 8ll * e, out[r]);
       }
     }
   }
@@ -116,29 +179,70 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
   __shared__ float red[T / 64], red3[3][T / 64];
   __shared__ float4 join[T == 64 ? 6 * CH * 64 : 1];
   constexpr int TEAMS = T == 64 ? 4 : 1;
-  const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, wave = threadIdx.x >> 6, n = a.K / 8;
+  // What every row of the sample is multiplied with, (1 + scale) w and the gate, in LDS: in registers it would be 16 a share, and one
+  // wavefront per SIMD less.  Of four shares it would not fit: read anew every row.
+  constexpr bool HELD = CH <= 3, AHEAD = CH <= 2 || (CH == 3 && !GATE);
+  __shared__ float4 up[HELD ? 2 * T * CH : 1], gates[HELD && GATE ? 2 * T * CH : 1];
+  const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = a.K / 8;
   const long long K = a.K;
   const float inv = 1.0f / (float)a.K;
   const int s = blockIdx.x / chunks, j = blockIdx.x - s * chunks;
   const long long first = (long long)s * a.rows + (long long)j * per;
   const long long last = min((long long)a.M, min((long long)(s + 1) * a.rows, first + per));
-  float a0[CH][8] = {}, a1[CH][8] = {}, a2[GATE ? CH : 1][8] = {};
-  for (long long m = first + (T == 64 ? wave : 0); m < last; m += TEAMS) {
-    // The vectors are the same in every row: they stay in registers, 20 a share, but where a thread has four shares (`again` hides
-    // that they are; and res is then read where it is needed).
-    int again = 0;
-    if constexpr (CH > 3) asm volatile("" : "+s"(again));
-    uint4 rg[CH], rx[CH], rh[CH], rr[CH];
+  // (1 + scale) w, and the gate, of share e
+  auto up_of = [&](int e, float (&v)[8]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      rg[c] = rx[c] = rh[c] = rr[c] = uint4{0u, 0u, 0u, 0u};
-      if (t + c * T < n) {
-        rg[c] = load_from<NT, uint4>(a.dy + m * K + 8ll * (t + c * T));
-        rx[c] = load_from<NT, uint4>(a.h + m * K + 8ll * (t + c * T));
-        if (a.dh) rh[c] = load_from<NT, uint4>(a.dh + m * K + 8ll * (t + c * T));
-        if (GATE && CH <= 3 && a.res) rr[c] = load_from<NT, uint4>(a.res + m * K + 8ll * (t + c * T));
+    for (int i = 0; i < 8; ++i) v[i] = 1.0f;
+    float u[8];
+    if (a.scale.v) {
+      load8(a.scale.v + s * a.scale.stride + 8 * e, u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += u[i];
+    }
+    if (a.w) {
+      unpack8(*(const uint4*)(a.w + 8 * e), u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= u[i];
+    }
+  };
+  auto held = [&](const float4* from, int e, float (&v)[8]) __attribute__((always_inline)) {   // (in two halves: no bank twice)
+    const float4 x = from[e], y = from[T * CH + e];
+    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+  };
+  if constexpr (HELD) {
+    for (int e = threadIdx.x; e < n; e += TEAMS * T) {
+      float v[8];
+      up_of(e, v);
+      up[e] = float4{v[0], v[1], v[2], v[3]};
+      up[T * CH + e] = float4{v[4], v[5], v[6], v[7]};
+      if constexpr (GATE) {
+        load8(a.gate.v + s * a.gate.stride + 8 * e, v);
+        gates[e] = float4{v[0], v[1], v[2], v[3]};
+        gates[T * CH + e] = float4{v[4], v[5], v[6], v[7]};
       }
     }
+    __syncthreads();
+  }
+  float a0[CH][8] = {}, a1[CH][8] = {}, a2[GATE ? CH : 1][8] = {};
+  struct Row { uint4 g[CH], x[CH], h[CH], r[CH]; };
+  auto load = [&](long long m, Row& w) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      w.g[c] = w.x[c] = w.h[c] = w.r[c] = uint4{0u, 0u, 0u, 0u};
+      if (t + c * T < n) {
+        w.g[c] = load_from<NT, uint4>(a.dy + m * K + 8ll * (t + c * T));
+        w.x[c] = load_from<NT, uint4>(a.h + m * K + 8ll * (t + c * T));
+        if (a.dh) w.h[c] = load_from<NT, uint4>(a.dh + m * K + 8ll * (t + c * T));
+        if (GATE && HELD && a.res) w.r[c] = load_from<NT, uint4>(a.res + m * K + 8ll * (t + c * T));
+      }
+    }
+  };
+  auto row = [&](long long m, Row& w, Row& ahead) __attribute__((always_inline)) {
+    uint4 (&rg)[CH] = w.g, (&rx)[CH] = w.x, (&rh)[CH] = w.h, (&rr)[CH] = w.r;
+    int again = 0;                       // (where the vectors are not held: hides that they are the same in every row)
+    if constexpr (!HELD) asm volatile("" : "+s"(again));
+    if (AHEAD && m + TEAMS < last) load(m + TEAMS, ahead);
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -148,28 +252,24 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
       for (int i = 0; i < 8; ++i) sum += x[i];
     }
     const float mean = team_sum<T>(sum, red) * inv;
-    // of one share: h - mean and g = dy o (1 + scale) o w, both zero where there are no features
+    // of one share: h - mean and g = dy o (1 + scale) o w
     auto share = [&](int c, float (&x)[8], float (&g)[8]) __attribute__((always_inline)) {
-      const int e = min(t + c * T, n - 1) + again;
+      const int e = t + c * T;
+      float u[8];
+      if constexpr (HELD) held(up, e, u);
+      else up_of(e + again, u);
       unpack8(rx[c], x);
       unpack8(rg[c], g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = t + c * T < n ? x[i] - mean : 0.f;
-      float u[8];
-      if (a.scale.v) {
-        load8(a.scale.v + s * a.scale.stride + 8 * e, u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = __builtin_fmaf(g[i], u[i], g[i]);
-      }
-      if (a.w) {
-        unpack8(*(const uint4*)(a.w + 8 * e), u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] *= u[i];
+      for (int i = 0; i < 8; ++i) {
+        x[i] -= mean;
+        g[i] *= u[i];
       }
     };
     float ss = 0.f, sg = 0.f, xg = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
+      if (t + c * T >= n) break;
       float x[8], g[8];
       share(c, x, g);
 #pragma unroll
@@ -194,8 +294,11 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int e = t + c * T;
+      if (e >= n) break;
       float x[8], g[8], d[8], u[8];
-      if (GATE && CH > 3 && a.res && e < n) rr[c] = load_from<NT, uint4>(a.res + m * K + 8ll * e);
+      // (h - mean and g are formed again from the packed words: kept, they would be 16 registers a share)
+      asm volatile("" : "+v"(rx[c].x), "+v"(rx[c].y), "+v"(rx[c].z), "+v"(rx[c].w), "+v"(rg[c].x), "+v"(rg[c].y), "+v"(rg[c].z), "+v"(rg[c].w));
+      if (GATE && !HELD && a.res) rr[c] = load_from<NT, uint4>(a.res + m * K + 8ll * e);
       share(c, x, g);
       unpack8(rg[c], u);
 #pragma unroll
@@ -206,20 +309,31 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
       unpack8(rh[c], d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) d[i] = __builtin_fmaf(__builtin_fmaf(-x[i], dot, g[i] - mg), r, d[i]);
-      if (e < n) store_to<NT>(a.dx + m * K + 8ll * e, pack8(d));
+      store_to<NT>(a.dx + m * K + 8ll * e, pack8(d));
       if constexpr (GATE) {
         unpack8(rr[c], u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) a2[c][i] = __builtin_fmaf(d[i], u[i], a2[c][i]);
-        if (a.dres && e < n) {
-          load8(a.gate.v + s * a.gate.stride + 8 * (e + again), u);
+        if (a.dres) {
+          if constexpr (HELD) held(gates, e, u);
+          else load8(a.gate.v + s * a.gate.stride + 8 * (e + again), u);
 #pragma unroll
           for (int i = 0; i < 8; ++i) d[i] *= u[i];
           store_to<NT>(a.dres + m * K + 8ll * e, pack8(d));
         }
       }
-      if constexpr (CH > 3) __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_sched_barrier(0);
     }
+  };
+  Row r0, r1;
+  long long m = first + (T == 64 ? wave : 0);
+  if (AHEAD && m < last) load(m, r0);
+  for (; m < last; m += AHEAD ? 2 * TEAMS : TEAMS) {
+    if (!AHEAD) load(m, r0);
+    row(m, r0, r1);
+    if (!AHEAD) continue;
+    if (m + TEAMS >= last) break;
+    row(m + TEAMS, r1, r0);
   }
   auto f4 = [](const float* x) __attribute__((always_inline)) { return float4{x[0], x[1], x[2], x[3]}; };
   auto leave = [&](float* to, const float (&acc)[CH][8], float4* mine) __attribute__((always_inline)) {
@@ -265,45 +379,65 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
 }
 
 // A sample's sums from its workgroups' shares, in a fixed order, and the gradients they give: workgroup (sample, 64 columns),
-// 16 threads of four adjacent columns, 16 along the shares.  With several samples, what each adds to dw and db goes to
-// pw, pb [samples, K], which launch_sum_partials adds up.
+// 16 threads of four adjacent columns, 64 along the shares: bound by the latency of a few rounds of loads.  With several samples, what
+// each adds to dw and db goes to pw, pb [samples, K], which launch_sum_partials adds up.
 constexpr int LSUM_ENTRIES = 64;
-__global__ void __launch_bounds__(256) layer_sums_kernel(LayerBwdArgs a, int chunks, const float* s0, const float* s1,
-                                                         const float* s2, float* pw, float* pb) {
-  __shared__ float4 red[3][16][16];
+__global__ void __launch_bounds__(1024) layer_sums_kernel(LayerBwdArgs a, int chunks, const float* s0, const float* s1,
+                                                          const float* s2, float* pw, float* pb) {
+  __shared__ float4 red[3][64][16];
   const int blocks = (a.K + LSUM_ENTRIES - 1) / LSUM_ENTRIES, s = blockIdx.x / blocks;
   const int t = threadIdx.x, col = t & 15, row = t >> 4, x = (blockIdx.x - s * blocks) * LSUM_ENTRIES + 4 * col;
   auto add = [](float4& a, const float4& b) __attribute__((always_inline)) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; };
   const float* src[3] = {s0, s1, s2};
+  float4 v[3] = {};
+  if (x < a.K) {
+    for (int p = row; p < chunks; p += 128) {
+      float4 u[3][2] = {};
+      const bool two = p + 64 < chunks;
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    float4 v[4] = {};
-    if (src[k] && x < a.K) {
-      const float* part = src[k] + (long long)s * chunks * a.K + x;
-      int p = row;
-      for (; p + 48 < chunks; p += 64)
+      for (int k = 0; k < 3; ++k) {
+        if (!src[k]) continue;
+        const float* part = src[k] + ((long long)s * chunks + p) * a.K + x;
+        u[k][0] = *(const float4*)part;
+        if (two) u[k][1] = *(const float4*)(part + 64ll * a.K);
+      }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) add(v[u], *(const float4*)(part + (long long)(p + 16 * u) * a.K));
-      for (; p < chunks; p += 16) add(v[0], *(const float4*)(part + (long long)p * a.K));
+      for (int k = 0; k < 3; ++k) {
+        add(u[k][0], u[k][1]);
+        add(v[k], u[k][0]);
+      }
     }
-    add(v[0], v[1]);
-    add(v[2], v[3]);
-    add(v[0], v[2]);
-    red[k][row][col] = v[0];
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) red[k][row][col] = v[k];
+  __syncthreads();
+  if (row < 48) {                             // kind row / 16: rows r, r + 16, r + 32, r + 48 into row r
+    const int k = row >> 4, r = row & 15;
+    float4 w = red[k][r][col], y = red[k][r + 32][col];
+    add(w, red[k][r + 16][col]);
+    add(y, red[k][r + 48][col]);
+    add(w, y);
+    red[k][r][col] = w;
+  }
+  __syncthreads();
+  if (row < 12) {
+    const int k = row >> 2, r = row & 3;
+    float4 w = red[k][r][col], y = red[k][r + 8][col];
+    add(w, red[k][r + 4][col]);
+    add(y, red[k][r + 12][col]);
+    add(w, y);
+    red[k][r][col] = w;
   }
   __syncthreads();
   if (t >= 16 || x >= a.K) return;
   float4 sum[3];
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    float4 r[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = red[k][i][t];
-#pragma unroll
-    for (int step = 1; step < 16; step *= 2)
-#pragma unroll
-      for (int i = 0; i < 16; i += 2 * step) add(r[i], r[i + step]);
-    sum[k] = r[0];
+    sum[k] = red[k][0][t];
+    float4 y = red[k][2][t];
+    add(sum[k], red[k][1][t]);
+    add(y, red[k][3][t]);
+    add(sum[k], y);
   }
   const long long at = (long long)s * a.K + x;
   const float v0[4] = {sum[0].x, sum[0].y, sum[0].z, sum[0].w}, v1[4] = {sum[1].x, sum[1].y, sum[1].z, sum[1].w};
@@ -364,27 +498,35 @@ static bool streams(int M, int K, int tensors) { return (long long)M * K * 2 * t
 
 void launch_layer_fwd(const LayerArgs& a, hipStream_t stream) {
   const bool nt = streams(a.M, a.K, a.res ? 4 : 2);
-#define LAYER_FWD(T, CH)                                                                  \
-  do {                                                                                    \
-    const unsigned grid = (unsigned)min(T == 64 ? (a.M + 3) / 4 : a.M, 1 << 20);          \
-    constexpr int threads = T == 64 ? 256 : T;                                            \
-    if (a.codes) {                                                                        \
-      if (nt) layer_fwd_kernel<T, CH, true, true><<<grid, threads, 0, stream>>>(a);       \
-      else layer_fwd_kernel<T, CH, true, false><<<grid, threads, 0, stream>>>(a);         \
-    } else {                                                                              \
-      if (nt) layer_fwd_kernel<T, CH, false, true><<<grid, threads, 0, stream>>>(a);      \
-      else layer_fwd_kernel<T, CH, false, false><<<grid, threads, 0, stream>>>(a);        \
-    }                                                                                     \
+  const int rows = min(a.rows, a.M);
+  // Two rows at a time share the vectors (75600 x 5120 601 -> 541 us, 20000 x 8192 256 -> 232, 20000 x 13824 414 -> 404), where there are so many
+  // that the chip is full all the same (1000 x 5120 11.5 / 12.2, 1000 x 1536 6.6 / 7.8); a wavefront's rows only on their way into codes, two of
+  // which are a line (65520 x 1536 -> 8960 612 -> 598; 65520 x 1536 by itself 141 / 143).
+  const bool two = rows > 1 && a.M >= 4096 && (a.codes || (a.K > 2048 && (a.gate.v || a.scale.v || a.shift.v)));
+  const int per_sample = two ? (rows + 1) / 2 : rows, whole = a.M / rows, left = a.M - whole * rows;
+  const int groups = whole * per_sample + (two ? (left + 1) / 2 : left);
+#define LAYER_FWD_(T, CH, ROWS, MX, NT) \
+  layer_fwd_kernel<T, CH, ROWS, MX, NT><<<(unsigned)(T == 64 ? (groups + 3) / 4 : groups), T == 64 ? 256 : T, 0, stream>>>(a, groups, per_sample)
+#define LAYER_FWD(T, CH)                                                                                       \
+  do {                                                                                                         \
+    if (a.codes) {                                                                                             \
+      if (two) { if (nt) LAYER_FWD_(T, CH, 2, true, true); else LAYER_FWD_(T, CH, 2, true, false); }           \
+      else { if (nt) LAYER_FWD_(T, CH, 1, true, true); else LAYER_FWD_(T, CH, 1, true, false); }               \
+    } else {                                                                                                   \
+      if (two) { if (nt) LAYER_FWD_(T, CH, 2, false, true); else LAYER_FWD_(T, CH, 2, false, false); }         \
+      else { if (nt) LAYER_FWD_(T, CH, 1, false, true); else LAYER_FWD_(T, CH, 1, false, false); }             \
+    }                                                                                                          \
   } while (0)
   LAYER_TEAMS(a.codes ? mx_steps(a.K) * (MX_STEP / 8) : a.K / 8, LAYER_FWD);   // (codes: those behind the last feature too)
 #undef LAYER_FWD
+#undef LAYER_FWD_
 }
 
 // How a sample's rows are dealt: at least eight to a workgroup (to a team), but enough workgroups to fill the chip.
 struct LayerDeal { int samples, chunks, per; };
 static LayerDeal layer_deal(int M, int K, int rows) {
   rows = min(rows, M);
-  const int samples = (M + rows - 1) / rows, teams = K <= 2048 ? 4 : 1, most = K <= 8192 ? 1024 : 512;
+  const int samples = (M + rows - 1) / rows, teams = K <= 2048 ? 4 : 1, most = K <= 8192 ? 512 : 256;
   const int all = (rows + teams - 1) / teams;                              // chunks of one row per team
   const int want = max(1, (min(most, max(most / 2, M / (8 * teams))) + samples - 1) / samples);
   const int per = teams * ((all + min(all, want) - 1) / min(all, want));
@@ -424,7 +566,7 @@ void launch_layer_bwd(const LayerBwdArgs& a, hipStream_t stream) {
     pw = g.w ? (float*)(ws + 3 * one) : nullptr;
     pb = g.b ? (float*)(ws + 3 * one + per_sample) : nullptr;
   }
-  layer_sums_kernel<<<(unsigned)d.samples * ((a.K + LSUM_ENTRIES - 1) / LSUM_ENTRIES), 256, 0, stream>>>(a, d.chunks, s0, s1, s2, pw, pb);
+  layer_sums_kernel<<<(unsigned)d.samples * ((a.K + LSUM_ENTRIES - 1) / LSUM_ENTRIES), 1024, 0, stream>>>(a, d.chunks, s0, s1, s2, pw, pb);
   if (d.samples > 1 && (g.w || g.b)) {
     PartialSums p{};
     p.part[0] = pw; p.dw[0] = g.w; p.width[0] = a.K;
