@@ -7,33 +7,34 @@
 namespace sla {
 
 // ---------------------------------------------------------------------------
-// A wavefront takes 512 features of ROWS rows, eight features a lane: four lanes are a block.
-template <int ROWS>
-__global__ void __launch_bounds__(256) mxfp4_quantize_kernel(const bf16_t* __restrict__ x, int R, int K, int RP, int KB,
+// A wavefront takes a step (256 features) of 2 PAIRS rows, two rows at a time, eight features a lane: four lanes are a block, and two
+// rows' records are a whole line.  NT: what is read or written once and exceeds the memory-side cache goes past the caches.
+template <int PAIRS, bool NT>
+__global__ void __launch_bounds__(256) mxfp4_quantize_kernel(const bf16_t* __restrict__ x, int R, int K, int RP, int KB, int units,
                                                              uint8_t* __restrict__ codes, uint8_t* __restrict__ exps) {
-  const int halves = (KB + 1) / 2, unit = (int)blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int group = unit / halves, k8 = (unit - group * halves) * 64 + lane, r0 = group * ROWS;
-  if (r0 >= R || k8 >= KB * (MX_STEP / 8)) return;
-  uint4 v[ROWS];
+  const int unit = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  if (unit >= units) return;
+  const int group = unit / KB, k8 = (unit - group * KB) * 32 + (lane & 31), r0 = group * 2 * PAIRS + (lane >> 5);
+  uint4 v[PAIRS];
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
+  for (int i = 0; i < PAIRS; ++i) {
     v[i] = uint4{0u, 0u, 0u, 0u};
-    if (r0 + i < R && k8 < K / 8) v[i] = *(const uint4*)(x + (long long)(r0 + i) * K + 8ll * k8);
+    if (r0 + 2 * i < R && k8 < K / 8) v[i] = load_from<NT, uint4>(x + (long long)(r0 + 2 * i) * K + 8ll * k8);
   }
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i)
-    if (r0 + i < R) mx_store8(v[i], r0 + i, k8, RP, codes, exps);
+  for (int i = 0; i < PAIRS; ++i)
+    if (r0 + 2 * i < R) mx_store8(v[i], r0 + 2 * i, k8, RP, codes, exps);   // (a quad is one row's)
 }
 
-// Eight features a thread.
-__global__ void __launch_bounds__(256) mxfp4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ exps,
-                                                               int R, int K, int RP, bf16_t* __restrict__ x) {
-  const int halves = (K / 8 + 63) / 64, unit = (int)blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int row = unit / halves, k8 = (unit - row * halves) * 64 + lane;
-  if (row >= R || k8 >= K / 8) return;
-  const int kb = k8 >> 5, c = (k8 >> 2) & 7;
-  const uint32_t four = *(const uint32_t*)(codes + mx_chunk_at(RP, row, kb, c) + 4 * (k8 & 3));
-  const uint32_t e = exps[mx_exp_at(RP, row, kb, c)];
+// What eight codes of a block of exponent e stand for, as bf16.
+__device__ __forceinline__ uint4 mx_values8(uint32_t four, uint32_t e) {
+  if (e - 1u < 252u) {                        // (the scale a normal number, no value beyond bf16: exact)
+    const float s = __uint_as_float(e << 23);
+    return uint4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(four, s, 0)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(four, s, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(four, s, 2)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(four, s, 3))};
+  }
   float v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -42,7 +43,24 @@ __global__ void __launch_bounds__(256) mxfp4_dequantize_kernel(const uint8_t* __
     const float twice = m < 4 ? (float)m : (float)((4 + 2 * (m & 1)) << ((m >> 1) - 2));
     v[i] = e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(__float_as_uint(ldexpf(twice, (int)e - 128)) | sign);
   }
-  *(uint4*)(x + (long long)row * K + 8ll * k8) = pack8(v);
+  return pack8(v);
+}
+template <int PAIRS, bool NT>
+__global__ void __launch_bounds__(256) mxfp4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ exps,
+                                                               int R, int K, int RP, int KB, int units, bf16_t* __restrict__ x) {
+  const int unit = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  if (unit >= units) return;
+  const int group = unit / KB, kb = unit - group * KB, k8 = kb * 32 + (lane & 31), r0 = group * 2 * PAIRS + (lane >> 5), c = (k8 >> 2) & 7;
+  uint32_t v[PAIRS], e[PAIRS];
+#pragma unroll
+  for (int i = 0; i < PAIRS; ++i) {           // (rows behind the last: what lies there, not stored)
+    const int row = min(r0 + 2 * i, RP - 1);
+    v[i] = *(const uint32_t*)(codes + mx_chunk_at(RP, row, kb, c) + 4 * (k8 & 3));
+    e[i] = exps[mx_exp_at(RP, row, kb, c)];
+  }
+#pragma unroll
+  for (int i = 0; i < PAIRS; ++i)
+    if (r0 + 2 * i < R && k8 < K / 8) store_to<NT>(x + (long long)(r0 + 2 * i) * K + 8ll * k8, mx_values8(v[i], e[i]));
 }
 
 // One block of 32 features a thread.
@@ -622,15 +640,23 @@ static void launch_tiles(const uint8_t* x, const uint8_t* xe, const uint8_t* w, 
 }
 
 // ---------------------------------------------------------------------------
+// Sixteen rows a wavefront, two where that would leave compute units without work.
+#define MX_ROWS(KERNEL, ...)                                                                                          \
+  do {                                                                                                                \
+    const int KB = mx_steps(K), pairs = (long long)((R + 15) / 16) * KB >= 4096 ? 8 : 1;                              \
+    const int units = (R + 2 * pairs - 1) / (2 * pairs) * KB;                                                         \
+    const unsigned grid = (unsigned)((units + 3) / 4);                                                                \
+    if (pairs == 1) KERNEL<1, false><<<grid, 256, 0, stream>>>(__VA_ARGS__);                                          \
+    else if ((long long)R * K * 2 > (256ll << 20)) KERNEL<8, true><<<grid, 256, 0, stream>>>(__VA_ARGS__);            \
+    else KERNEL<8, false><<<grid, 256, 0, stream>>>(__VA_ARGS__);                                                     \
+  } while (0)
 void launch_mxfp4_quantize(const void* x, int R, int K, uint8_t* codes, uint8_t* exps, hipStream_t stream) {
-  const int KB = mx_steps(K);
-  const long long units = (long long)((R + 7) / 8) * ((KB + 1) / 2);
-  mxfp4_quantize_kernel<8><<<(unsigned)((units + 3) / 4), 256, 0, stream>>>((const bf16_t*)x, R, K, mx_rows(R), KB, codes, exps);
+  MX_ROWS(mxfp4_quantize_kernel, (const bf16_t*)x, R, K, mx_rows(R), KB, units, codes, exps);
 }
 void launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* exps, int R, int K, void* x, hipStream_t stream) {
-  const long long units = (long long)R * ((K / 8 + 63) / 64);
-  mxfp4_dequantize_kernel<<<(unsigned)((units + 3) / 4), 256, 0, stream>>>(codes, exps, R, K, mx_rows(R), (bf16_t*)x);
+  MX_ROWS(mxfp4_dequantize_kernel, codes, exps, R, K, mx_rows(R), KB, units, (bf16_t*)x);
 }
+#undef MX_ROWS
 void launch_mxfp4_pack(const uint8_t* from, const uint8_t* from_exps, int R, int K, uint8_t* codes, uint8_t* exps, hipStream_t stream) {
   mxfp4_pack_kernel<<<2048, 256, 0, stream>>>(from, from_exps, R, K, mx_rows(R), mx_steps(K), codes, exps);
 }
@@ -662,13 +688,15 @@ void launch_mxfp4_gemm(const uint8_t* x, const uint8_t* xe, const uint8_t* w, co
     return;
   }
 #define MX_ARGS x, xe, w, we, bias, y, M, N, K, stream
+  if (M <= 64) {
+    if (M > 32) return launch_split<1, 2, 4>(MX_ARGS);
+    if (K > 16 * MX_STEP) return launch_split<1, 1, 8>(MX_ARGS);
+    return launch_split<1, 1, 4>(MX_ARGS);
+  }
   if (tiles(256, 128) >= 512) return launch_tiles<4, 1, 2, 4, 3, 2>(MX_ARGS);
   if (tiles(128, 128) > 256) return launch_tiles<2, 2, 2, 2, 3, 3>(MX_ARGS);
   if (tiles(128, 128) >= 64) return launch_tiles<2, 2, 2, 2, 4, 2>(MX_ARGS);
-  if (M > 64) return launch_split<2, 2, 4>(MX_ARGS);
-  if (M > 32) return launch_split<1, 2, 4>(MX_ARGS);
-  if (K > 16 * MX_STEP) return launch_split<1, 1, 8>(MX_ARGS);
-  launch_split<1, 1, 4>(MX_ARGS);
+  launch_split<2, 2, 4>(MX_ARGS);
 #undef MX_ARGS
 }
 
