@@ -886,49 +886,100 @@ def w8a8_norm_linear_fwd(x, norm_w, wq, N, res=None, eps=1e-6, bias=None, worksp
     return out, x if res is None else h
 
 
+# ---------------------------------------------------------------------------
+# The layer norm of include/norm.h
+# ---------------------------------------------------------------------------
+# As above, and shorter still: a tensor is checked once, its device by number; what a function has made itself is not checked.
+def _go(name, device, *args):
+    """Calls the C entry point `name` with args and the current stream of the device of that number, made the current one
+    where it is not."""
+    f = getattr(lib(), name)
+    if device == torch.cuda.current_device():
+        st = f(*args, torch._C._cuda_getCurrentRawStream(device))
+    else:
+        with torch.cuda.device(device):
+            st = f(*args, torch._C._cuda_getCurrentRawStream(device))
+    if st != SLA_OK:
+        raise SLAError(st, name)
+
+
+def _matrix(x, what):
+    """(rows, features, number of its CUDA device) of a contiguous bfloat16 matrix."""
+    device = x.get_device()
+    if x.dtype is not torch.bfloat16 or x.dim() != 2 or device < 0 or not x.is_contiguous():
+        raise ValueError("%s: expected a contiguous 2-D CUDA bfloat16 tensor" % what)
+    M, K = x.shape
+    return M, K, device
+
+
+def _of(t, what, shape, device, dtype=torch.bfloat16):
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous %s tensor of %r on the CUDA device of the other tensors" % (what, dtype, shape))
+    return t.data_ptr()
+
+
+def _maybe(t, what, shape, device):
+    return None if t is None else _of(t, what, shape, device)
+
+
+def _bytes_on(t, what, device):
+    """A caller's object or workspace (whose size the library checks)."""
+    if t.dtype is not torch.uint8 or t.get_device() != device or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous uint8 tensor on the CUDA device of the other tensors" % what)
+    return t.data_ptr()
+
+
 LayerGrads = collections.namedtuple("LayerGrads", "dx dres dw dbias dgate dscale dshift")
 
 
-def _modulation(M, K, gate, scale, shift):
+def _modulation(M, K, device, gate, scale, shift):
     """(norm_modulation or None, samples) of the samples' vectors, each fp32 [samples, K] with contiguous features."""
-    S = 0
+    S, at = 0, []
     for t, what in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
         if t is None:
+            at += [(None, 0)]
             continue
-        if t.dtype != torch.float32 or not t.is_cuda or t.dim() != 2 or t.shape[1] != K or t.stride(1) != 1:
-            raise ValueError("%s: expected a CUDA float32 tensor [samples, %d] with contiguous features" % (what, K))
-        if t.shape[0] < 1 or M % t.shape[0] or (S and t.shape[0] != S):
+        if t.dtype is not torch.float32 or t.dim() != 2 or t.shape[1] != K or t.stride(1) != 1 or t.get_device() != device:
+            raise ValueError("%s: expected a float32 tensor [samples, %d] with contiguous features on the CUDA device of the other "
+                             "tensors" % (what, K))
+        n = t.shape[0]
+        if n < 1 or M % n or (S and n != S):
             raise ValueError("gate, scale and shift: one number of samples, of M / samples rows each")
-        S = t.shape[0]
+        S = n
+        at += [(t.data_ptr(), t.stride(0) if n > 1 else 0)]         # (of one sample the stride says nothing)
     if S == 0:
         return None, 1
-    st = [0 if t is None or S == 1 else t.stride(0) for t in (gate, scale, shift)]    # (of one sample the stride says nothing)
-    return NormModulation(_at(gate), _at(scale), _at(shift), *st, M // S), S
+    (g, gs), (c, cs), (h, hs) = at
+    return NormModulation(g, c, h, gs, cs, hs, M // S), S
 
 
 def _layer_args(x, w, bias, res, gate, scale, shift, h):
-    """(M, K, h, modulation) of a layer norm's forward direction."""
-    M, K = _rows_of(x, "x")
-    _vector(w, "w", K)
-    _vector(bias, "bias", K)
+    """(M, K, device, h, the arguments up to h) of a layer norm's forward direction."""
+    M, K, device = _matrix(x, "x")
+    mod, _ = _modulation(M, K, device, gate, scale, shift)
+    h_at = None
     if res is not None:
-        _rows_of(res, "res", (M, K))
-        h = torch.empty_like(x) if h is None else h
-        _rows_of(h, "h", (M, K))
+        if h is None:
+            h = torch.empty_like(x)
+            h_at = h.data_ptr()
+        else:
+            h_at = _of(h, "h", (M, K), device)
     elif h is not None or gate is not None:
         raise ValueError("h is written, and a gate applied, only where there is a res")
-    return M, K, h, _modulation(M, K, gate, scale, shift)[0]
+    return M, K, device, x if res is None else h, (x.data_ptr(), _maybe(res, "res", (M, K), device), _maybe(w, "w", (K,), device),
+                                                   _maybe(bias, "bias", (K,), device), _by_ref(mod), h_at)
 
 
 def norm_layer_fwd(x, w=None, bias=None, res=None, gate=None, scale=None, shift=None, eps=1e-6, out=None, h=None):
     """(y, h): h = x + gate o res in bf16 (x itself without res), y = (n o w + bias) o (1 + scale) + shift with n the layer norm
     of h.  w, bias: bf16 [K]; gate, scale, shift: fp32 [samples, K] in any stride, each sample M / samples consecutive rows."""
-    M, K, h, mod = _layer_args(x, w, bias, res, gate, scale, shift, h)
-    out = torch.empty_like(x) if out is None else out
-    _rows_of(out, "out", (M, K))
-    _launch("norm_layer_fwd", x.device, (w, bias, res, gate, scale, shift, out, h), _at(x), _at(res), _at(w), _at(bias),
-            _by_ref(mod), _at(h), _at(out), M, K, eps)
-    return out, x if res is None else h
+    M, K, device, h, args = _layer_args(x, w, bias, res, gate, scale, shift, h)
+    if out is None:
+        out = torch.empty_like(x)
+    else:
+        _of(out, "out", (M, K), device)
+    _go("norm_layer_fwd", device, *args, out.data_ptr(), M, K, eps)
+    return out, h
 
 
 def norm_layer_bwd_workspace_bytes(M, K, rows):
@@ -940,32 +991,28 @@ def norm_layer_bwd(dy, h, w=None, bias=None, dh=None, res=None, gate=None, scale
     """LayerGrads of norm_layer_fwd, h being the stored stream; dh: the gradient that h has from elsewhere.  There is a gradient of
     each of w, bias, gate (with res), scale and shift that is given, in fp32 (of the last three per sample), unless want_vectors
     is False; dres is None without a gate: it is dx then."""
-    M, K = _rows_of(dy, "dy")
-    _rows_of(h, "h", (M, K))
-    _vector(w, "w", K)
-    _vector(bias, "bias", K)
-    for t, what in ((dh, "dh"), (res, "res")):
-        if t is not None:
-            _rows_of(t, what, (M, K))
-    mod, S = _modulation(M, K, gate, scale, shift)
-    dx = torch.empty_like(dy) if dx is None else dx
-    _rows_of(dx, "dx", (M, K))
-    if gate is not None:
-        dres = torch.empty_like(dy) if dres is None else dres
-        _rows_of(dres, "dres", (M, K))
-    elif dres is not None:
+    M, K, device = _matrix(dy, "dy")
+    one = (M, K)
+    mod, S = _modulation(M, K, device, gate, scale, shift)
+    if dres is not None and gate is None:
         raise ValueError("dres is written only where there is a gate")
     if want_vectors and gate is not None and res is None:
         raise ValueError("the gate's gradient needs res")
+    at = (dy.data_ptr(), _maybe(dh, "dh", one, device), _of(h, "h", one, device), _maybe(res, "res", one, device),
+          _maybe(w, "w", (K,), device), _maybe(bias, "bias", (K,), device), _by_ref(mod))
+    dx = torch.empty_like(dy) if dx is None else dx
+    _of(dx, "dx", one, device)
+    if gate is not None:
+        dres = torch.empty_like(dy) if dres is None else dres
+        _of(dres, "dres", one, device)
     new = lambda t, *shape: torch.empty(shape, dtype=torch.float32, device=dy.device) if want_vectors and t is not None else None
     dw, db, dgate, dscale, dshift = new(w, K), new(bias, K), new(gate, S, K), new(scale, S, K), new(shift, S, K)
-    grads = None
+    grads, ws, ws_bytes = None, None, 0
     if any(t is not None for t in (dw, db, dgate, dscale, dshift)):
         grads = NormLayerGrads(_at(dw), _at(db), _at(dgate), _at(dscale), _at(dshift))
         workspace = _scratch(workspace, norm_layer_bwd_workspace_bytes(M, K, M // S), dy.device, "norm_layer_bwd")
-    _launch("norm_layer_bwd", dy.device, (h, w, bias, dh, res, gate, scale, shift, dx, dres, workspace), _at(dy), _at(dh), _at(h),
-            _at(res), _at(w), _at(bias), _by_ref(mod), _at(dx), _at(dres), _by_ref(grads), M, K, eps, _at(workspace),
-            0 if workspace is None else workspace.numel())
+        ws, ws_bytes = _bytes_on(workspace, "workspace", device), workspace.numel()
+    _go("norm_layer_bwd", device, *at, dx.data_ptr(), _at(dres), _by_ref(grads), M, K, eps, ws, ws_bytes)
     return LayerGrads(dx, dres, dw, db, dgate, dscale, dshift)
 
 
@@ -976,99 +1023,108 @@ def mxfp4_bytes(R, K):
     return lib().mxfp4_bytes(R, K)
 
 
-def _mx_object(q, R, K, what):
-    if q.dtype != torch.uint8 or not q.is_cuda or not q.is_contiguous() or q.numel() < max(1, mxfp4_bytes(R, K)):
-        raise ValueError("%s: expected the object of an [%d, %d] matrix" % (what, R, K))
+def _object_for(q, R, K, like, device, where):
+    """(the caller's object or workspace or a new one of an [R, K] matrix, its address, its bytes)"""
+    q = _scratch(q, mxfp4_bytes(R, K) if q is None else 0, like.device, where)
+    return q, _bytes_on(q, "object or workspace", device), q.numel()
 
 
 def mxfp4_quantize(x, q=None):
     """The object (a uint8 tensor) of x bf16 [R, K], weights [N, K] and activations [M, K] alike."""
-    R, K = _rows_of(x, "x")
-    q = _scratch(q, mxfp4_bytes(R, K), x.device, "mxfp4_quantize")
-    _launch("mxfp4_quantize", x.device, (q,), _at(x), R, K, _at(q), q.numel())
+    R, K, device = _matrix(x, "x")
+    q, at, nbytes = _object_for(q, R, K, x, device, "mxfp4_quantize")
+    _go("mxfp4_quantize", device, x.data_ptr(), R, K, at, nbytes)
     return q
 
 
 def mxfp4_dequantize(q, R, K, out=None):
     """What the codes of an object stand for, bf16 [R, K]."""
-    _mx_object(q, R, K, "q")
-    out = torch.empty((R, K), dtype=torch.bfloat16, device=q.device) if out is None else out
-    _rows_of(out, "out", (R, K))
-    _launch("mxfp4_dequantize", q.device, (out,), _at(q), q.numel(), R, K, _at(out))
+    device = q.get_device()
+    at = _bytes_on(q, "q", max(device, 0))
+    if out is None:
+        out = torch.empty((R, K), dtype=torch.bfloat16, device=q.device)
+    _go("mxfp4_dequantize", device, at, q.numel(), R, K, _of(out, "out", (R, K), device))
     return out
-
-
-def _bytes_2d(t, what, shape):
-    if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
-        raise ValueError("%s: expected a contiguous CUDA uint8 tensor of %r" % (what, shape))
 
 
 def mxfp4_pack(codes, exponents, q=None):
     """The object of plain rows: codes uint8 [R, K / 2] (two features a byte, the first in the low half), exponents uint8
     [R, ceil(K / 32)]."""
+    device = max(codes.get_device(), 0)
+    if codes.dim() != 2:
+        raise ValueError("codes: expected a uint8 tensor [R, K / 2]")
     R, K = codes.shape[0], 2 * codes.shape[1]
-    _bytes_2d(codes, "codes", (R, K // 2))
-    _bytes_2d(exponents, "exponents", (R, -(-K // 32)))
-    q = _scratch(q, mxfp4_bytes(R, K), codes.device, "mxfp4_pack")
-    _launch("mxfp4_pack", codes.device, (exponents, q), _at(codes), _at(exponents), R, K, _at(q), q.numel())
+    c = _of(codes, "codes", (R, K // 2), device, torch.uint8)
+    e = _of(exponents, "exponents", (R, -(-K // 32)), device, torch.uint8)
+    q, at, nbytes = _object_for(q, R, K, codes, device, "mxfp4_pack")
+    _go("mxfp4_pack", device, c, e, R, K, at, nbytes)
     return q
 
 
 def mxfp4_unpack(q, R, K):
     """(codes, exponents) of an object as mxfp4_pack takes them."""
-    _mx_object(q, R, K, "q")
+    device = max(q.get_device(), 0)
+    at = _bytes_on(q, "q", device)
     codes = torch.empty((R, K // 2), dtype=torch.uint8, device=q.device)
     exponents = torch.empty((R, -(-K // 32)), dtype=torch.uint8, device=q.device)
-    _launch("mxfp4_unpack", q.device, (), _at(q), q.numel(), R, K, _at(codes), _at(exponents))
+    _go("mxfp4_unpack", device, at, q.numel(), R, K, codes.data_ptr(), exponents.data_ptr())
     return codes, exponents
 
 
-def _mx_out(wq, bias, out, M, N, K, device):
-    """The result's tensor, weight and bias checked."""
-    _mx_object(wq, N, K, "wq")
-    _vector(bias, "bias", N)
-    out = torch.empty((M, N), dtype=torch.bfloat16, device=device) if out is None else out
-    _rows_of(out, "out", (M, N))
-    return out
+def _layer_result(out, M, N, x, device):
+    if out is None:
+        out = x.new_empty((M, N)) if x.dtype is torch.bfloat16 else torch.empty((M, N), dtype=torch.bfloat16, device=x.device)
+        return out, out.data_ptr()
+    return out, _of(out, "out", (M, N), device)
+
+
+def _layer_workspace(workspace, M, K, x, device, where):
+    """(the tensor, its address, its bytes) of a caller's workspace or a new one."""
+    if workspace is not None:
+        return workspace, _bytes_on(workspace, "workspace", device), workspace.numel()
+    nbytes = mxfp4_bytes(M, K)
+    if nbytes == 0:
+        raise ValueError("unsupported problem for %s" % where)
+    workspace = x.new_empty(nbytes // 2)          # (of 16 bits like x: made fastest)
+    return workspace, workspace.data_ptr(), nbytes
 
 
 def mxfp4_gemm_fwd(xq, wq, M, N, K, bias=None, out=None):
     """y bf16 [M, N] of the objects of activations [M, K] and a weight [N, K]."""
-    _mx_object(xq, M, K, "xq")
-    out = _mx_out(wq, bias, out, M, N, K, xq.device)
-    _launch("mxfp4_gemm_fwd", xq.device, (wq, bias, out), _at(xq), xq.numel(), _at(wq), wq.numel(), _at(bias), _at(out), M, N, K)
+    device = max(xq.get_device(), 0)
+    x_at, w_at = _bytes_on(xq, "xq", device), _bytes_on(wq, "wq", device)
+    out, at = _layer_result(out, M, N, xq, device)
+    _go("mxfp4_gemm_fwd", device, x_at, xq.numel(), w_at, wq.numel(), _maybe(bias, "bias", (N,), device), at, M, N, K)
     return out
 
 
 def mxfp4_linear_fwd(x, wq, N, bias=None, workspace=None, out=None):
     """y bf16 [M, N] of x bf16 [M, K], quantised on the way, and the object `wq` of an [N, K] weight."""
-    M, K = _rows_of(x, "x")
-    workspace = _scratch(workspace, mxfp4_bytes(M, K), x.device, "mxfp4_linear_fwd")
-    out = _mx_out(wq, bias, out, M, N, K, x.device)
-    _launch("mxfp4_linear_fwd", x.device, (wq, bias, out, workspace), _at(x), _at(wq), wq.numel(), _at(bias), _at(out), M, N, K,
-            _at(workspace), workspace.numel())
+    M, K, device = _matrix(x, "x")
+    w_at = _bytes_on(wq, "wq", device)
+    workspace, ws, ws_bytes = _layer_workspace(workspace, M, K, x, device, "mxfp4_linear_fwd")
+    out, at = _layer_result(out, M, N, x, device)
+    _go("mxfp4_linear_fwd", device, x.data_ptr(), w_at, wq.numel(), _maybe(bias, "bias", (N,), device), at, M, N, K, ws, ws_bytes)
     return out
 
 
 def mxfp4_norm_quantize(x, w=None, bias=None, res=None, gate=None, scale=None, shift=None, eps=1e-6, q=None, h=None):
     """(q, h): the object of norm_layer_fwd's y, which is not written."""
-    M, K, h, mod = _layer_args(x, w, bias, res, gate, scale, shift, h)
-    q = _scratch(q, mxfp4_bytes(M, K), x.device, "mxfp4_norm_quantize")
-    _launch("mxfp4_norm_quantize", x.device, (w, bias, res, gate, scale, shift, h, q), _at(x), _at(res), _at(w), _at(bias),
-            _by_ref(mod), _at(h), _at(q), q.numel(), M, K, eps)
-    return q, x if res is None else h
+    M, K, device, h, args = _layer_args(x, w, bias, res, gate, scale, shift, h)
+    q, at, nbytes = _object_for(q, M, K, x, device, "mxfp4_norm_quantize")
+    _go("mxfp4_norm_quantize", device, *args, at, nbytes, M, K, eps)
+    return q, h
 
 
 def mxfp4_norm_linear_fwd(x, wq, N, norm_w=None, norm_bias=None, res=None, gate=None, scale=None, shift=None, eps=1e-6, bias=None,
                           workspace=None, h=None, out=None):
     """(y, h): y bf16 [M, N] = the 4-bit layer of norm_layer_fwd's y, with the object `wq` of an [N, K] weight."""
-    M, K, h, mod = _layer_args(x, norm_w, norm_bias, res, gate, scale, shift, h)
-    workspace = _scratch(workspace, mxfp4_bytes(M, K), x.device, "mxfp4_norm_linear_fwd")
-    out = _mx_out(wq, bias, out, M, N, K, x.device)
-    _launch("mxfp4_norm_linear_fwd", x.device, (norm_w, norm_bias, res, gate, scale, shift, h, wq, bias, out, workspace), _at(x),
-            _at(res), _at(norm_w), _at(norm_bias), _by_ref(mod), _at(h), _at(wq), wq.numel(), _at(bias), _at(out), M, N, K, eps,
-            _at(workspace), workspace.numel())
-    return out, x if res is None else h
+    M, K, device, h, args = _layer_args(x, norm_w, norm_bias, res, gate, scale, shift, h)
+    w_at = _bytes_on(wq, "wq", device)
+    workspace, ws, ws_bytes = _layer_workspace(workspace, M, K, x, device, "mxfp4_norm_linear_fwd")
+    out, at = _layer_result(out, M, N, x, device)
+    _go("mxfp4_norm_linear_fwd", device, *args, w_at, wq.numel(), _maybe(bias, "bias", (N,), device), at, M, N, K, eps, ws, ws_bytes)
+    return out, h
 
 
 # ---------------------------------------------------------------------------

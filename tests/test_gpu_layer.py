@@ -105,7 +105,7 @@ def test_every_vector_by_itself():
     every = sla.norm_layer_bwd(dy, h, **v)
     wanted = {"w": "dw", "b": "dbias", "gate": "dgate", "scale": "dscale", "shift": "dshift"}
     ws = torch.empty(sla.norm_layer_bwd_workspace_bytes(S * rows, K, rows), dtype=torch.uint8, device="cuda")
-    mod, _ = sla._modulation(S * rows, K, v["gate"], v["scale"], v["shift"])
+    mod, _ = sla._modulation(S * rows, K, 0, v["gate"], v["scale"], v["shift"])
     for name, grad in wanted.items():
         like = getattr(every, grad)
         out, dx = torch.full_like(like, 7.0), torch.empty_like(dy)
@@ -142,7 +142,7 @@ def test_a_last_sample_that_is_shorter():
     """Through the C entry points: rows per sample need not divide the number of rows."""
     M, rows, K = 23, 10, 136
     r, x, v = _inputs(3, 10, K, "all")
-    mod, _ = sla._modulation(30, K, v["gate"], v["scale"], v["shift"])
+    mod, _ = sla._modulation(30, K, 0, v["gate"], v["scale"], v["shift"])
     full = sla.norm_layer_fwd(x, **v)
     y, h = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
     at = lambda t: t.data_ptr()
