@@ -21,7 +21,15 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs 
   __shared__ float red[2][ROWS][T / 64];
   constexpr int TEAMS = T == 64 ? 4 : 1;
   const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = a.K / 8;
-  const int group = TEAMS * blockIdx.x + (T == 64 ? wave : 0);
+  int block = blockIdx.x;
+  if constexpr (MX) {
+    // Workgroups are dealt round-robin over the 8 XCDs: of every 8 RUN, RUN neighbours to each, so that the 16 rows whose exponents
+    // share a line are one L2's.
+    constexpr int RUN = 16 / (ROWS * TEAMS);
+    const int from = block / (8 * RUN) * (8 * RUN);
+    if (from + 8 * RUN <= (int)gridDim.x) block = from + ((block - from) & 7) * RUN + ((block - from) >> 3);
+  }
+  const int group = TEAMS * block + (T == 64 ? wave : 0);
   if (group >= groups) return;                 // (T > 64: the whole workgroup)
   const long long K = a.K;
   const float inv = 1.0f / (float)a.K;
@@ -478,6 +486,8 @@ __global__ void __launch_bounds__(1024) layer_sums_kernel(LayerBwdArgs a, int ch
     else if (n_ <= 640) F(320, 2);        \
     else if (n_ <= 768) F(384, 2);        \
     else if (n_ <= 1024) F(512, 2);       \
+    else if (n_ <= 1280) F(640, 2);       \
+    else if (n_ <= 1536) F(768, 2);       \
     else F(1024, 2);                      \
   } while (0)
 #define LAYER_BWD_TEAMS(n, F)             \
