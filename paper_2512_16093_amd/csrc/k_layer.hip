@@ -14,6 +14,10 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
 
+// Share e of a row: its address is the row's, the same for a wavefront, and 32 bits of each lane's.
+__device__ __forceinline__ const bf16_t* share_of(const bf16_t* row, int e) { return (const bf16_t*)((const char*)row + 16u * (unsigned)e); }
+__device__ __forceinline__ bf16_t* share_of(bf16_t* row, int e) { return (bf16_t*)((char*)row + 16u * (unsigned)e); }
+
 // MX: codes instead of y.  A team takes ROWS rows of one sample at a time: two share what they read of the vectors, which come from the
 // caches, 12 bytes a feature with a gate, scale and shift.
 template <int T, int CH, int ROWS, bool MX, bool NT>
@@ -64,8 +68,8 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs 
     for (int c = 0; c < CH; ++c) {
       v[r][c] = add[r][c] = uint4{0u, 0u, 0u, 0u};
       if (t + c * T < n) {
-        v[r][c] = load_from<NT, uint4>(a.x + row(r) * K + 8ll * (t + c * T));
-        if (a.res) add[r][c] = load_from<NT, uint4>(a.res + row(r) * K + 8ll * (t + c * T));
+        v[r][c] = load_from<NT, uint4>(share_of(a.x + row(r) * K, t + c * T));
+        if (a.res) add[r][c] = load_from<NT, uint4>(share_of(a.res + row(r) * K, t + c * T));
       }
     }
   // The vectors: of a lone wavefront requested before they are needed, behind what is waited for first, the rows and the sums (65520 x 1536
@@ -107,7 +111,7 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs 
           for (int i = 0; i < 8; ++i) x[i] += u[i];
         }
         v[r][c] = pack8(x);
-        if (there(r)) store_to<NT>(a.h + row(r) * K + 8ll * e, v[r][c]);
+        if (there(r)) store_to<NT>(share_of(a.h + row(r) * K, e), v[r][c]);
         unpack8(v[r][c], x);
       }
 #pragma unroll
@@ -173,7 +177,7 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs 
       if constexpr (MX) {
         if (e < mx_steps(a.K) * (MX_STEP / 8) && there(r)) mx_store8(out[r], (int)row(r), e, mx_rows(a.M), a.codes, a.exps);
       } else {
-        if (e < n && there(r)) store_to<NT>(a.y + row(r) * K + 8ll * e, out[r]);
+        if (e < n && there(r)) store_to<NT>(share_of(a.y + row(r) * K, e), out[r]);
       }
     }
   }
@@ -187,21 +191,22 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
   __shared__ float red[T / 64], red3[3][T / 64];
   __shared__ float4 join[T == 64 ? 6 * CH * 64 : 1];
   constexpr int TEAMS = T == 64 ? 4 : 1;
-  // What every row of the sample is multiplied with, (1 + scale) w and the gate, in LDS: in registers it would be 16 a share, and one
-  // wavefront per SIMD less.  Of four shares it would not fit: read anew every row.
-  constexpr bool HELD = CH <= 3, AHEAD = CH <= 2 || (CH == 3 && !GATE);
-  __shared__ float4 up[HELD ? 2 * T * CH : 1], gates[HELD && GATE ? 2 * T * CH : 1];
+  // What every row of the sample is multiplied with, (1 + scale) w and the gate, in LDS, each in two halves (no bank twice): in registers
+  // it would be 16 a share, and one wavefront per SIMD less.
+  // AHEAD: the next row is requested while this one is worked on, where there are registers for it (20000 x 4096 234 -> 219 us; three shares
+  // with a gate would have one wavefront per SIMD less: 65520 x 1536 256 -> 267).
+  constexpr bool AHEAD = T <= 512 && (CH <= 2 || (CH == 3 && !GATE));
+  __shared__ float4 up[2 * T * CH], gates[GATE ? 2 * T * CH : 1];
   const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = a.K / 8;
   const long long K = a.K;
   const float inv = 1.0f / (float)a.K;
   const int s = blockIdx.x / chunks, j = blockIdx.x - s * chunks;
   const long long first = (long long)s * a.rows + (long long)j * per;
   const long long last = min((long long)a.M, min((long long)(s + 1) * a.rows, first + per));
-  // (1 + scale) w, and the gate, of share e
-  auto up_of = [&](int e, float (&v)[8]) __attribute__((always_inline)) {
+  for (int e = threadIdx.x; e < n; e += TEAMS * T) {
+    float v[8], u[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = 1.0f;
-    float u[8];
     if (a.scale.v) {
       load8(a.scale.v + s * a.scale.stride + 8 * e, u);
 #pragma unroll
@@ -212,26 +217,15 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= u[i];
     }
-  };
-  auto held = [&](const float4* from, int e, float (&v)[8]) __attribute__((always_inline)) {   // (in two halves: no bank twice)
-    const float4 x = from[e], y = from[T * CH + e];
-    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-    v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-  };
-  if constexpr (HELD) {
-    for (int e = threadIdx.x; e < n; e += TEAMS * T) {
-      float v[8];
-      up_of(e, v);
-      up[e] = float4{v[0], v[1], v[2], v[3]};
-      up[T * CH + e] = float4{v[4], v[5], v[6], v[7]};
-      if constexpr (GATE) {
-        load8(a.gate.v + s * a.gate.stride + 8 * e, v);
-        gates[e] = float4{v[0], v[1], v[2], v[3]};
-        gates[T * CH + e] = float4{v[4], v[5], v[6], v[7]};
-      }
+    up[e] = float4{v[0], v[1], v[2], v[3]};
+    up[T * CH + e] = float4{v[4], v[5], v[6], v[7]};
+    if constexpr (GATE) {
+      load8(a.gate.v + s * a.gate.stride + 8 * e, v);
+      gates[e] = float4{v[0], v[1], v[2], v[3]};
+      gates[T * CH + e] = float4{v[4], v[5], v[6], v[7]};
     }
-    __syncthreads();
   }
+  __syncthreads();
   float a0[CH][8] = {}, a1[CH][8] = {}, a2[GATE ? CH : 1][8] = {};
   struct Row { uint4 g[CH], x[CH], h[CH], r[CH]; };
   auto load = [&](long long m, Row& w) __attribute__((always_inline)) {
@@ -239,17 +233,15 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
     for (int c = 0; c < CH; ++c) {
       w.g[c] = w.x[c] = w.h[c] = w.r[c] = uint4{0u, 0u, 0u, 0u};
       if (t + c * T < n) {
-        w.g[c] = load_from<NT, uint4>(a.dy + m * K + 8ll * (t + c * T));
-        w.x[c] = load_from<NT, uint4>(a.h + m * K + 8ll * (t + c * T));
-        if (a.dh) w.h[c] = load_from<NT, uint4>(a.dh + m * K + 8ll * (t + c * T));
-        if (GATE && HELD && a.res) w.r[c] = load_from<NT, uint4>(a.res + m * K + 8ll * (t + c * T));
+        w.g[c] = load_from<NT, uint4>(share_of(a.dy + m * K, t + c * T));
+        w.x[c] = load_from<NT, uint4>(share_of(a.h + m * K, t + c * T));
+        if (a.dh) w.h[c] = load_from<NT, uint4>(share_of(a.dh + m * K, t + c * T));
+        if (GATE && a.res) w.r[c] = load_from<NT, uint4>(share_of(a.res + m * K, t + c * T));
       }
     }
   };
   auto row = [&](long long m, Row& w, Row& ahead) __attribute__((always_inline)) {
     uint4 (&rg)[CH] = w.g, (&rx)[CH] = w.x, (&rh)[CH] = w.h, (&rr)[CH] = w.r;
-    int again = 0;                       // (where the vectors are not held: hides that they are the same in every row)
-    if constexpr (!HELD) asm volatile("" : "+s"(again));
     if (AHEAD && m + TEAMS < last) load(m + TEAMS, ahead);
     float sum = 0.f;
 #pragma unroll
@@ -260,31 +252,47 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
       for (int i = 0; i < 8; ++i) sum += x[i];
     }
     const float mean = team_sum<T>(sum, red) * inv;
-    // of one share: h - mean and g = dy o (1 + scale) o w
-    auto share = [&](int c, float (&x)[8], float (&g)[8]) __attribute__((always_inline)) {
-      const int e = t + c * T;
-      float u[8];
-      if constexpr (HELD) held(up, e, u);
-      else up_of(e + again, u);
-      unpack8(rx[c], x);
-      unpack8(rg[c], g);
+    auto unpack4 = [](uint32_t lo, uint32_t hi, float (&v)[4]) __attribute__((always_inline)) {
+      v[0] = bf16_lo(lo); v[1] = bf16_hi(lo); v[2] = bf16_lo(hi); v[3] = bf16_hi(hi);
+    };
+    auto held = [&](const float4* from, int c, int q, float (&v)[4]) __attribute__((always_inline)) {
+      const float4 x = from[q * T * CH + t + c * T];
+      v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    };
+    // of half a share: h - mean, dy, and g = dy o (1 + scale) o w
+    auto half = [&](int c, int q, float (&x)[4], float (&y)[4], float (&g)[4]) __attribute__((always_inline)) {
+      float u[4];
+      held(up, c, q, u);
+      // (formed anew from the packed words each time: kept, they would be 16 registers a share)
+      if (q == 0) {
+        asm volatile("" : "+v"(rx[c].x), "+v"(rx[c].y), "+v"(rg[c].x), "+v"(rg[c].y));
+        unpack4(rx[c].x, rx[c].y, x);
+        unpack4(rg[c].x, rg[c].y, y);
+      } else {
+        asm volatile("" : "+v"(rx[c].z), "+v"(rx[c].w), "+v"(rg[c].z), "+v"(rg[c].w));
+        unpack4(rx[c].z, rx[c].w, x);
+        unpack4(rg[c].z, rg[c].w, y);
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 4; ++i) {
         x[i] -= mean;
-        g[i] *= u[i];
+        g[i] = y[i] * u[i];
       }
     };
     float ss = 0.f, sg = 0.f, xg = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       if (t + c * T >= n) break;
-      float x[8], g[8];
-      share(c, x, g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        ss = __builtin_fmaf(x[i], x[i], ss);
-        sg += g[i];
-        xg = __builtin_fmaf(x[i], g[i], xg);
+      for (int q = 0; q < 2; ++q) {
+        float x[4], y[4], g[4];
+        half(c, q, x, y, g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ss = __builtin_fmaf(x[i], x[i], ss);
+          sg += g[i];
+          xg = __builtin_fmaf(x[i], g[i], xg);
+        }
       }
     }
     ss = rows_sum(row_sum(ss));
@@ -303,33 +311,36 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
     for (int c = 0; c < CH; ++c) {
       const int e = t + c * T;
       if (e >= n) break;
-      float x[8], g[8], d[8], u[8];
-      // (h - mean and g are formed again from the packed words: kept, they would be 16 registers a share)
-      asm volatile("" : "+v"(rx[c].x), "+v"(rx[c].y), "+v"(rx[c].z), "+v"(rx[c].w), "+v"(rg[c].x), "+v"(rg[c].y), "+v"(rg[c].z), "+v"(rg[c].w));
-      if (GATE && !HELD && a.res) rr[c] = load_from<NT, uint4>(a.res + m * K + 8ll * e);
-      share(c, x, g);
-      unpack8(rg[c], u);
+      uint32_t dx[4], dr[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        a0[c][i] += u[i];
-        a1[c][i] = __builtin_fmaf(u[i], x[i] * r, a1[c][i]);
-      }
-      unpack8(rh[c], d);
+      for (int q = 0; q < 2; ++q) {
+        float x[4], y[4], g[4], d[4];
+        half(c, q, x, y, g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) d[i] = __builtin_fmaf(__builtin_fmaf(-x[i], dot, g[i] - mg), r, d[i]);
-      store_to<NT>(a.dx + m * K + 8ll * e, pack8(d));
-      if constexpr (GATE) {
-        unpack8(rr[c], u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a2[c][i] = __builtin_fmaf(d[i], u[i], a2[c][i]);
-        if (a.dres) {
-          if constexpr (HELD) held(gates, e, u);
-          else load8(a.gate.v + s * a.gate.stride + 8 * (e + again), u);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) d[i] *= u[i];
-          store_to<NT>(a.dres + m * K + 8ll * e, pack8(d));
+        for (int i = 0; i < 4; ++i) {
+          a0[c][4 * q + i] += y[i];
+          a1[c][4 * q + i] = __builtin_fmaf(y[i], x[i] * r, a1[c][4 * q + i]);
         }
-      }
+        unpack4(q ? rh[c].z : rh[c].x, q ? rh[c].w : rh[c].y, d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = __builtin_fmaf(__builtin_fmaf(-x[i], dot, g[i] - mg), r, d[i]);
+        dx[2 * q] = pack_bf16x2(d[0], d[1]);
+        dx[2 * q + 1] = pack_bf16x2(d[2], d[3]);
+        if constexpr (GATE) {
+          unpack4(q ? rr[c].z : rr[c].x, q ? rr[c].w : rr[c].y, y);
+          held(gates, c, q, g);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            a2[c][4 * q + i] = __builtin_fmaf(d[i], y[i], a2[c][4 * q + i]);
+            d[i] *= g[i];
+          }
+          dr[2 * q] = pack_bf16x2(d[0], d[1]);
+          dr[2 * q + 1] = pack_bf16x2(d[2], d[3]);
+        }
+        }
+      store_to<NT>(share_of(a.dx + m * K, e), uint4{dx[0], dx[1], dx[2], dx[3]});
+      if constexpr (GATE)
+        if (a.dres) store_to<NT>(share_of(a.dres + m * K, e), uint4{dr[0], dr[1], dr[2], dr[3]});
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -500,7 +511,8 @@ __global__ void __launch_bounds__(1024) layer_sums_kernel(LayerBwdArgs a, int ch
     else if (n_ <= 512) F(256, 2);        \
     else if (n_ <= 768) F(256, 3);        \
     else if (n_ <= 1024) F(512, 2);       \
-    else F(512, 4);                       \
+    else if (gate) F(512, 4);             \
+    else F(768, 3);                       \
   } while (0)
 
 // `tensors` of these that do not fit the memory-side cache together are read and written past it.
@@ -560,7 +572,10 @@ void launch_layer_bwd(const LayerBwdArgs& a, hipStream_t stream) {
 #define LAYER_BWD(T, CH)                                                                                            \
   do {                                                                                                              \
     constexpr int threads = T == 64 ? 256 : T;                                                                      \
-    if (gate) {                                                                                                     \
+    if constexpr (T == 768) {   /* (never with a gate: there three shares do not fit the registers) */               \
+      if (nt) layer_bwd_kernel<T, CH, false, true><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);   \
+      else layer_bwd_kernel<T, CH, false, false><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);     \
+    } else if (gate) {                                                                                              \
       if (nt) layer_bwd_kernel<T, CH, true, true><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);    \
       else layer_bwd_kernel<T, CH, true, false><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);      \
     } else {                                                                                                        \
