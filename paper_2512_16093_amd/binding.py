@@ -893,8 +893,8 @@ def w8a8_norm_linear_fwd(x, norm_w, wq, N, res=None, eps=1e-6, bias=None, worksp
 def _go(name, device, *args):
     """Calls the C entry point `name` with args and the current stream of the device of that number, made the current one
     where it is not."""
-    f = getattr(lib(), name)
-    if device == torch.cuda.current_device():
+    f = getattr(_lib or lib(), name)
+    if device == torch._C._cuda_getDevice():
         st = f(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
         with torch.cuda.device(device):
@@ -1020,13 +1020,18 @@ def norm_layer_bwd(dy, h, w=None, bias=None, dh=None, res=None, gate=None, scale
 # include/mxfp4.h
 # ---------------------------------------------------------------------------
 def mxfp4_bytes(R, K):
-    return lib().mxfp4_bytes(R, K)
+    return (_lib or lib()).mxfp4_bytes(R, K)
 
 
 def _object_for(q, R, K, like, device, where):
-    """(the caller's object or workspace or a new one of an [R, K] matrix, its address, its bytes)"""
-    q = _scratch(q, mxfp4_bytes(R, K) if q is None else 0, like.device, where)
-    return q, _bytes_on(q, "object or workspace", device), q.numel()
+    """(the caller's object or a new one of an [R, K] matrix, its address, its bytes)"""
+    if q is not None:
+        return q, _bytes_on(q, "q", device), q.numel()
+    nbytes = mxfp4_bytes(R, K)
+    if nbytes == 0:
+        raise ValueError("unsupported problem for %s" % where)
+    q = like.new_empty(nbytes, dtype=torch.uint8)
+    return q, q.data_ptr(), nbytes
 
 
 def mxfp4_quantize(x, q=None):
@@ -1042,8 +1047,11 @@ def mxfp4_dequantize(q, R, K, out=None):
     device = q.get_device()
     at = _bytes_on(q, "q", max(device, 0))
     if out is None:
-        out = torch.empty((R, K), dtype=torch.bfloat16, device=q.device)
-    _go("mxfp4_dequantize", device, at, q.numel(), R, K, _of(out, "out", (R, K), device))
+        out = q.new_empty((R, K), dtype=torch.bfloat16)
+        out_at = out.data_ptr()
+    else:
+        out_at = _of(out, "out", (R, K), device)
+    _go("mxfp4_dequantize", device, at, q.numel(), R, K, out_at)
     return out
 
 
@@ -1073,7 +1081,7 @@ def mxfp4_unpack(q, R, K):
 
 def _layer_result(out, M, N, x, device):
     if out is None:
-        out = x.new_empty((M, N)) if x.dtype is torch.bfloat16 else torch.empty((M, N), dtype=torch.bfloat16, device=x.device)
+        out = x.new_empty((M, N), dtype=torch.bfloat16)
         return out, out.data_ptr()
     return out, _of(out, "out", (M, N), device)
 
