@@ -397,6 +397,31 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
   if constexpr (GATE) leave(s2, a2, join + (T == 64 ? 4 * CH * 64 : 0));
 }
 
+__device__ __forceinline__ void add4(float4& a, const float4& b) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; }
+// The gradients that the sums of sample s give in columns x .. x + 3: its vectors' are stored, what it adds to dw and db returned.
+__device__ __forceinline__ void layer_grads4(const LayerBwdArgs& a, int s, int x, const float4 (&sum)[3], float4& dw, float4& db) {
+  const long long at = (long long)s * a.K + x;
+  const float v0[4] = {sum[0].x, sum[0].y, sum[0].z, sum[0].w}, v1[4] = {sum[1].x, sum[1].y, sum[1].z, sum[1].w};
+  float up[4] = {1.f, 1.f, 1.f, 1.f}, w[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {}, ds[4];
+  if (a.scale.v) {
+    const float4 u = *(const float4*)(a.scale.v + s * a.scale.stride + x);
+    up[0] += u.x; up[1] += u.y; up[2] += u.z; up[3] += u.w;
+  }
+  auto four = [&](const bf16_t* p, float (&v)[4]) __attribute__((always_inline)) {
+    const uint2 q = *(const uint2*)(p + x);
+    v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
+  };
+  if (a.w) four(a.w, w);
+  if (a.b) four(a.b, b);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ds[i] = __builtin_fmaf(w[i], v1[i], b[i] * v0[i]);
+  if (a.grads.shift) *(float4*)(a.grads.shift + at) = sum[0];
+  if (a.grads.scale) *(float4*)(a.grads.scale + at) = float4{ds[0], ds[1], ds[2], ds[3]};
+  if (a.grads.gate) *(float4*)(a.grads.gate + at) = sum[2];
+  dw = float4{up[0] * v1[0], up[1] * v1[1], up[2] * v1[2], up[3] * v1[3]};
+  db = float4{up[0] * v0[0], up[1] * v0[1], up[2] * v0[2], up[3] * v0[3]};
+}
+
 // A sample's sums from its workgroups' shares, in a fixed order, and the gradients they give: workgroup (sample, 64 columns),
 // 16 threads of four adjacent columns, 64 along the shares: bound by the latency of a few rounds of loads.  With several samples, what
 // each adds to dw and db goes to pw, pb [samples, K], which launch_sum_partials adds up.
@@ -406,7 +431,6 @@ __global__ void __launch_bounds__(1024) layer_sums_kernel(LayerBwdArgs a, int ch
   __shared__ float4 red[3][64][16];
   const int blocks = (a.K + LSUM_ENTRIES - 1) / LSUM_ENTRIES, s = blockIdx.x / blocks;
   const int t = threadIdx.x, col = t & 15, row = t >> 4, x = (blockIdx.x - s * blocks) * LSUM_ENTRIES + 4 * col;
-  auto add = [](float4& a, const float4& b) __attribute__((always_inline)) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; };
   const float* src[3] = {s0, s1, s2};
   float4 v[3] = {};
   if (x < a.K) {
@@ -422,8 +446,8 @@ __global__ void __launch_bounds__(1024) layer_sums_kernel(LayerBwdArgs a, int ch
       }
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
-        add(u[k][0], u[k][1]);
-        add(v[k], u[k][0]);
+        add4(u[k][0], u[k][1]);
+        add4(v[k], u[k][0]);
       }
     }
   }
@@ -433,18 +457,18 @@ __global__ void __launch_bounds__(1024) layer_sums_kernel(LayerBwdArgs a, int ch
   if (row < 48) {                             // kind row / 16: rows r, r + 16, r + 32, r + 48 into row r
     const int k = row >> 4, r = row & 15;
     float4 w = red[k][r][col], y = red[k][r + 32][col];
-    add(w, red[k][r + 16][col]);
-    add(y, red[k][r + 48][col]);
-    add(w, y);
+    add4(w, red[k][r + 16][col]);
+    add4(y, red[k][r + 48][col]);
+    add4(w, y);
     red[k][r][col] = w;
   }
   __syncthreads();
   if (row < 12) {
     const int k = row >> 2, r = row & 3;
     float4 w = red[k][r][col], y = red[k][r + 8][col];
-    add(w, red[k][r + 4][col]);
-    add(y, red[k][r + 12][col]);
-    add(w, y);
+    add4(w, red[k][r + 4][col]);
+    add4(y, red[k][r + 12][col]);
+    add4(w, y);
     red[k][r][col] = w;
   }
   __syncthreads();
@@ -454,34 +478,40 @@ __global__ void __launch_bounds__(1024) layer_sums_kernel(LayerBwdArgs a, int ch
   for (int k = 0; k < 3; ++k) {
     sum[k] = red[k][0][t];
     float4 y = red[k][2][t];
-    add(sum[k], red[k][1][t]);
-    add(y, red[k][3][t]);
-    add(sum[k], y);
+    add4(sum[k], red[k][1][t]);
+    add4(y, red[k][3][t]);
+    add4(sum[k], y);
   }
+  float4 dw, db;
+  layer_grads4(a, s, x, sum, dw, db);
   const long long at = (long long)s * a.K + x;
-  const float v0[4] = {sum[0].x, sum[0].y, sum[0].z, sum[0].w}, v1[4] = {sum[1].x, sum[1].y, sum[1].z, sum[1].w};
-  float up[4] = {1.f, 1.f, 1.f, 1.f}, w[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {}, ds[4], dw[4], db[4];
-  if (a.scale.v) {
-    const float4 u = *(const float4*)(a.scale.v + s * a.scale.stride + x);
-    up[0] += u.x; up[1] += u.y; up[2] += u.z; up[3] += u.w;
-  }
-  auto four = [&](const bf16_t* p, float (&v)[4]) __attribute__((always_inline)) {
-    const uint2 q = *(const uint2*)(p + x);
-    v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
-  };
-  if (a.w) four(a.w, w);
-  if (a.b) four(a.b, b);
+  if (pw) *(float4*)(pw + at) = dw;
+  if (pb) *(float4*)(pb + at) = db;
+}
+
+// The same where a sample has few shares (many samples, down to a modulation of each row): four columns a thread, every `parts`-th
+// sample, whose additions to dw and db it adds up on the way (pw, pb [parts, K]).
+constexpr int LSUM_COLUMNS = 1024;
+__global__ void __launch_bounds__(256) layer_samples_kernel(LayerBwdArgs a, int samples, int chunks, int parts, const float* s0,
+                                                            const float* s1, const float* s2, float* pw, float* pb) {
+  const int blocks = (a.K + LSUM_COLUMNS - 1) / LSUM_COLUMNS, part = blockIdx.x / blocks;
+  const int x = (blockIdx.x - part * blocks) * LSUM_COLUMNS + 4 * threadIdx.x;
+  if (x >= a.K) return;
+  const float* src[3] = {s0, s1, s2};
+  float4 dw{}, db{};
+  for (int s = part; s < samples; s += parts) {
+    float4 sum[3] = {}, w, b;
+    for (int p = 0; p < chunks; ++p)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    ds[i] = __builtin_fmaf(w[i], v1[i], b[i] * v0[i]);
-    dw[i] = up[i] * v1[i];
-    db[i] = up[i] * v0[i];
+      for (int k = 0; k < 3; ++k)
+        if (src[k]) add4(sum[k], *(const float4*)(src[k] + ((long long)s * chunks + p) * a.K + x));
+    layer_grads4(a, s, x, sum, w, b);
+    add4(dw, w);
+    add4(db, b);
   }
-  if (a.grads.shift) *(float4*)(a.grads.shift + at) = sum[0];
-  if (a.grads.scale) *(float4*)(a.grads.scale + at) = float4{ds[0], ds[1], ds[2], ds[3]};
-  if (a.grads.gate) *(float4*)(a.grads.gate + at) = sum[2];
-  if (pw) *(float4*)(pw + at) = float4{dw[0], dw[1], dw[2], dw[3]};
-  if (pb) *(float4*)(pb + at) = float4{db[0], db[1], db[2], db[3]};
+  const long long at = (long long)part * a.K + x;
+  if (pw) *(float4*)(pw + at) = dw;
+  if (pb) *(float4*)(pb + at) = db;
 }
 
 // ---------------------------------------------------------------------------
@@ -545,25 +575,30 @@ void launch_layer_fwd(const LayerArgs& a, hipStream_t stream) {
 }
 
 // How a sample's rows are dealt: at least eight to a workgroup (to a team), but enough workgroups to fill the chip.
-struct LayerDeal { int samples, chunks, per; };
+// many: so many samples of so few shares that layer_samples_kernel adds them up (whole backward pass in us, else / so: 300 x 5120 in 100
+// samples 57 / 26, 1000 x 1536 in 500 74 / 27, 8000 x 5120 in 64 135 / 121; 8 x 5120, one sample, 10.6 / 15.4); parts: of dw and db, before the
+// last step adds them up.
+struct LayerDeal { int samples, chunks, per, parts; bool many; };
 static LayerDeal layer_deal(int M, int K, int rows) {
   rows = min(rows, M);
   const int samples = (M + rows - 1) / rows, teams = K <= 2048 ? 4 : 1, most = K <= 8192 ? 512 : 256;
   const int all = (rows + teams - 1) / teams;                              // chunks of one row per team
   const int want = max(1, (min(most, max(most / 2, M / (8 * teams))) + samples - 1) / samples);
   const int per = teams * ((all + min(all, want) - 1) / min(all, want));
-  return {samples, (rows + per - 1) / per, per};
+  const int chunks = (rows + per - 1) / per;
+  const bool many = chunks == 1 || (chunks <= 8 && samples >= 32);
+  return {samples, chunks, per, many ? min(samples, 2048 / ((K + LSUM_COLUMNS - 1) / LSUM_COLUMNS)) : samples, many};
 }
-// three sums per workgroup, and each sample's share of dw and db
+// three sums per workgroup, and the parts of dw and db
 size_t layer_bwd_bytes(int M, int K, int rows) {
   const LayerDeal d = layer_deal(M, K, rows);
-  return 3 * align256((size_t)d.samples * d.chunks * K * 4) + (d.samples > 1 ? 2 * align256((size_t)d.samples * K * 4) : 0);
+  return 3 * align256((size_t)d.samples * d.chunks * K * 4) + (d.parts > 1 ? 2 * align256((size_t)d.parts * K * 4) : 0);
 }
 
 void launch_layer_bwd(const LayerBwdArgs& a, hipStream_t stream) {
   const LayerDeal d = layer_deal(a.M, a.K, a.rows);
   const norm_layer_grads& g = a.grads;
-  const size_t one = align256((size_t)d.samples * d.chunks * a.K * 4), per_sample = align256((size_t)d.samples * a.K * 4);
+  const size_t one = align256((size_t)d.samples * d.chunks * a.K * 4), part = align256((size_t)d.parts * a.K * 4);
   unsigned char* ws = (unsigned char*)a.ws;
   const bool sums = g.w || g.b || g.scale || g.shift;
   float *s0 = sums ? (float*)ws : nullptr, *s1 = sums ? (float*)(ws + one) : nullptr, *s2 = g.gate ? (float*)(ws + 2 * one) : nullptr;
@@ -587,16 +622,19 @@ void launch_layer_bwd(const LayerBwdArgs& a, hipStream_t stream) {
 #undef LAYER_BWD
   if (!sums && !g.gate) return;
   float *pw = g.w, *pb = g.b;
-  if (d.samples > 1) {
+  if (d.parts > 1) {
     pw = g.w ? (float*)(ws + 3 * one) : nullptr;
-    pb = g.b ? (float*)(ws + 3 * one + per_sample) : nullptr;
+    pb = g.b ? (float*)(ws + 3 * one + part) : nullptr;
   }
-  layer_sums_kernel<<<(unsigned)d.samples * ((a.K + LSUM_ENTRIES - 1) / LSUM_ENTRIES), 1024, 0, stream>>>(a, d.chunks, s0, s1, s2, pw, pb);
-  if (d.samples > 1 && (g.w || g.b)) {
+  if (d.many)
+    layer_samples_kernel<<<(unsigned)d.parts * ((a.K + LSUM_COLUMNS - 1) / LSUM_COLUMNS), 256, 0, stream>>>(a, d.samples, d.chunks, d.parts, s0, s1, s2, pw, pb);
+  else
+    layer_sums_kernel<<<(unsigned)d.samples * ((a.K + LSUM_ENTRIES - 1) / LSUM_ENTRIES), 1024, 0, stream>>>(a, d.chunks, s0, s1, s2, pw, pb);
+  if (d.parts > 1 && (g.w || g.b)) {
     PartialSums p{};
     p.part[0] = pw; p.dw[0] = g.w; p.width[0] = a.K;
     p.part[1] = pb; p.dw[1] = g.b; p.width[1] = a.K;
-    p.n_part = d.samples;
+    p.n_part = d.parts;
     launch_sum_partials(p, stream);
   }
 }
