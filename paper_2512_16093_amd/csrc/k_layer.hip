@@ -2,7 +2,12 @@
 // (include/mxfp4.h) as well.
 //
 // A team of T threads per row, as in k_norm.hip: the row stays in registers between its sums and its result, so every tensor
-// is read or written once: bound by HBM.  Mean first, then the sum of the squared deviations from it.
+// is read or written once: bound by HBM (a copy reaches 4.9 TB/s, an addition of two tensors 5.8).  Mean first, then the sum of the
+// squared deviations from it: two passes over registers, no difference of large squares.  All in fp32; the stored stream is rounded to bf16
+// before it is normed, because its readers find it so, the result once.
+// Measured: forward with gate and modulation 75600 x 5120 541 us, 5.7 TB/s, 32760 x 5120 239, 65520 x 1536 145 (5.5), 20000 x 13824 404, without
+// residual 75600 x 5120 280 (5.5); into codes 75600 x 5120 456 (5.5), 65520 x 1536 115; one row of 5120 2.9.  Backward with everything
+// 65520 x 1536 252 us, 4.8 TB/s, 32760 x 5120 419 (4.8), 8192 x 5120 116, 129 x 1536 12.
 #include "layer.h"
 #include "mxfp4.h"
 
@@ -184,7 +189,8 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs 
 }
 
 // dx, dres, and each workgroup's shares of the sums over a sample's rows: S0 of dy, S1 of dy o n, S2 of dx o res, each
-// [workgroups, K].  Workgroup s * chunks + j takes rows j * per .. of sample s.
+// [workgroups, K] (all other sums over rows follow from these three: dw = (1 + scale) S1, db = (1 + scale) S0, dscale = w S1 + b S0,
+// dshift = S0, dgate = S2).  Workgroup s * chunks + j takes rows j * per .. of sample s.
 template <int T, int CH, bool GATE, bool NT>
 __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdArgs a, int chunks, int per, float* s0, float* s1,
                                                                        float* s2) {
@@ -515,7 +521,10 @@ __global__ void __launch_bounds__(256) layer_samples_kernel(LayerBwdArgs a, int 
 }
 
 // ---------------------------------------------------------------------------
-// The team and the shares of a thread for n shares of eight features: F(T, CH).
+// The team and the shares of a thread for n shares of eight features: F(T, CH).  Forward a wavefront per row up to K = 2048 (nothing
+// is exchanged), above that workgroups of two shares a thread, whose size follows the width so that few threads idle (20000 x 8960 277 -> 257 us
+// against 1024 threads from K = 8200 on, into codes 261 -> 230).  Backward the sums cost 8 to 24 registers a share: without a gate three shares
+// of 768 threads at most, with one four of 512 (20000 x 13824 838 -> 659 us, without a gate 474 -> 456, against 1024 threads of two).
 #define LAYER_TEAMS(n, F)                 \
   do {                                    \
     const int n_ = (n);                   \
@@ -545,7 +554,7 @@ __global__ void __launch_bounds__(256) layer_samples_kernel(LayerBwdArgs a, int 
     else F(768, 3);                       \
   } while (0)
 
-// `tensors` of these that do not fit the memory-side cache together are read and written past it.
+// `tensors` of these that do not fit the memory-side cache (256 MiB) together are read and written past it.
 static bool streams(int M, int K, int tensors) { return (long long)M * K * 2 * tensors > (256ll << 20); }
 
 void launch_layer_fwd(const LayerArgs& a, hipStream_t stream) {
@@ -574,7 +583,10 @@ void launch_layer_fwd(const LayerArgs& a, hipStream_t stream) {
 #undef LAYER_FWD_
 }
 
-// How a sample's rows are dealt: at least eight to a workgroup (to a team), but enough workgroups to fill the chip.
+// How a sample's rows are dealt: at least eight to a workgroup (to a team), but enough workgroups to fill the chip; more of them would only
+// leave more shares.  In us with at most 256 / 512 / 1024 workgroups (at least half of that): 1000 x 5120 33.1 / 29.8 / 31.4, 8192 x 5120
+// 125 / 116 / 128, 20000 x 5120 271 / 257 / 269, 65520 x 1536 253 / 256 / 250; with 128 / 256 / 512: 2048 x 13824 116 / 96 / 96, 8192 x 13824 395 / 288 /
+// 299.
 // many: so many samples of so few shares that layer_samples_kernel adds them up (whole backward pass in us, else / so: 300 x 5120 in 100
 // samples 57 / 26, 1000 x 1536 in 500 74 / 27, 8000 x 5120 in 64 135 / 121; 8 x 5120, one sample, 10.6 / 15.4); parts: of dw and db, before the
 // last step adds them up.
