@@ -523,7 +523,12 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
     pw += w_half;
     if (h % 2 == 0) pe += e_step;
   }
-  *(uint32_t*)(lds + AT_BIAS + wv * 256 + 4 * lane) = 0u;
+  // The bias of this wavefront's outputs, a tile ahead (without one what is there is copied, and not used).
+  const float* const from = (const float*)(bias ? (const void*)bias : (const void*)w);
+  auto copy_bias = [&](int n_) __attribute__((always_inline)) {
+    copy_floats(from, 2u * (unsigned)min(n_ * T::N + 32 * CT * wn + 2 * lane, N - 2), lds0 + AT_BIAS + wv * 256);
+  };
+  copy_bias(nt);
   copies_barrier<0>();
   v4i x0[RT], w0[CT], x1[RT], w1[CT];
   uint32_t xx[RT], wx[CT], xn[RT], wn_[CT];
@@ -531,13 +536,22 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
   for (int i = 0; i < OPS; ++i) read_one(0, 0, i, x0, w0);
 #pragma unroll
   for (int i = 0; i < OPS; ++i) read_exp(0, i, xx, wx);
+  // A tile's sums begin with the bias, by a product of its own: the bias as the first of 16 features, the tokens' a one.  (An addition of a
+  // word behind the last product would be 64 instructions more for every 32 tokens, when the matrix pipe has nothing to do.)
+  const uint32_t first_feature = hf == 0 ? 0xffffu : 0u, bias_mask = bias ? first_feature : 0u;
+  uint32_t bias_word[CT];
+  auto read_bias = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) bias_word[c] = *(const uint16_t*)(lds + AT_BIAS + wv * 256 + (32 * c + l32) * 2) & bias_mask;
+  };
+  read_bias();
   int stage = 0, eslot = 0;
   v16f acc[RT][CT];
 
-#define MX_PRODUCTS(KS, FIRST, X, W, AFTER)                                                           \
+#define MX_PRODUCTS(KS, X, W, AFTER)                                                           \
   _Pragma("unroll") for (int i = 0; i < PRODUCTS; ++i) {                                              \
     const int c = i / RT, r = i % RT;                                                                 \
-    acc[r][c] = mfma_mx<KS>(W[c], wx[c], X[r], xx[r], FIRST ? v16f{} : acc[r][c]);                    \
+    acc[r][c] = mfma_mx<KS>(W[c], wx[c], X[r], xx[r], acc[r][c]);                                     \
     (AFTER)(i);                                                                                       \
     __builtin_amdgcn_sched_barrier(0);                                                                \
   }
@@ -551,9 +565,9 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
       px = turn ? next_px : px; pw = turn ? next_pw : pw; pe = turn ? next_pe : pe;                   \
     }                                                                                                 \
     _Pragma("unroll") for (int i = 0; i < 2; ++i) read_one(stage, 1, i, x1, w1);                      \
-    MX_PRODUCTS(2 * PART, FIRST && PART == 0, x0, w0, [&](int i) { if (i + 2 < OPS) read_one(stage, 1, i + 2, x1, w1); })  \
+    MX_PRODUCTS(2 * PART, x0, w0, [&](int i) { if (i + 2 < OPS) read_one(stage, 1, i + 2, x1, w1); })  \
     copies_barrier<FIRST ? 63 : T::copies(PART + 2, PART + 2, 2)>();                                  \
-    MX_PRODUCTS(2 * PART + 1, false, x1, w1, [&](int i) {                                             \
+    MX_PRODUCTS(2 * PART + 1, x1, w1, [&](int i) {                                             \
       if (i < OPS) read_one(next, 0, i, x0, w0);                                                      \
       if (PART == 1 && i < OPS) read_exp(eslot ^ 1, i, xn, wn_);                                      \
       if (i >= 3 && i % 2 == 1 && (i - 3) / 2 < T::COPIES + PART) copy_one(stage, eslot, (i - 3) / 2);  \
@@ -574,15 +588,21 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
     tiles.at(more ? next_slot : slot, next_mt, next_nt);   // (behind the last tile its first halves once more, for nobody)
     const char *const next_px = x_at(next_mt), *const next_pw = w_at(next_nt), *const next_pe = e_at(next_mt, next_nt);
     const int n0 = nt * T::N + 32 * CT * wn;
-    if (bias) copy_floats((const float*)bias, 2u * (unsigned)min(n0 + 2 * lane, N - 2), lds0 + AT_BIAS + wv * 256);
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+        acc[r][c] = mfma_bf16(uint4{bias_word[c], 0u, 0u, 0u}, uint4{first_feature & 0x3f80u, 0u, 0u, 0u}, v16f{});
+    __builtin_amdgcn_sched_barrier(0);
     int step = 0;
     MX_HALF(0, true)
+    copy_bias(next_nt);                  // (its words have been read: the meeting in the half before waited for them)
     MX_HALF(1, true)
     for (step = 1; step < KB; ++step) {
       MX_HALF(0, false)
       MX_HALF(1, false)
     }
-    // Results: bias in, bf16, through LDS of their own so that rows leave as whole lines, past the caches.  The stores go by a buffer
+    // Results: bf16, through LDS of their own so that rows leave as whole lines, past the caches.  The stores go by a buffer
     // that ends with the last token and drops what lies behind its end: no branch may stand here, or the sums would be moved out of
     // their registers all at once.
     int ln = lane;
@@ -594,11 +614,6 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
     const uint64_t base = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(first >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)first);
     const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, __builtin_amdgcn_readfirstlane((int)left), 0x00020000);
     const unsigned at = n0 + 8 * part < N ? (unsigned)(ln >> 4) * (2u * (unsigned)N) + 2u * (n0 + 8 * part) : 0x80000000u;
-    uint2 bw[CT][4];
-#pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) bw[c][g] = *(const uint2*)(lds + AT_BIAS + wv * 256 + (32 * c + 8 * g + 4 * qh) * 2);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -608,14 +623,15 @@ __global__ void __launch_bounds__(256, 1) mxfp4_gemm_walk_kernel(const uint8_t* 
       for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const uint2 b4 = bw[c][g];
           const v16f& f = acc[r][c];
           *(uint2*)(my + q32 * T::EPI + (32 * c + 8 * g + 4 * qh) * 2) =
-              make_uint2(pack_bf16x2(f[4 * g] + bf16_lo(b4.x), f[4 * g + 1] + bf16_hi(b4.x)),
-                         pack_bf16x2(f[4 * g + 2] + bf16_lo(b4.y), f[4 * g + 3] + bf16_hi(b4.y)));
+              make_uint2(pack_bf16x2(f[4 * g], f[4 * g + 1]), pack_bf16x2(f[4 * g + 2], f[4 * g + 3]));
         }
       // (the next tile's first halves: waited for before the first result leaves, behind which they could not be told from it)
-      if (r == 0) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      if (r == 0) {
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        read_bias();
+      }
       __builtin_amdgcn_wave_barrier();   // (a wavefront's LDS operations execute in order: only the compiler has to keep it)
       v4i out[8];
 #pragma unroll
