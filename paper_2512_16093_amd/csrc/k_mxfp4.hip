@@ -463,8 +463,8 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
 // from tile to tile.  The operands of a product then come from LDS for sixteen others instead of eight, a byte copied from L2
 // serves 256 x 256 products of its feature, and nothing waits between tiles: the last half steps of one copy the first of the
 // next, whose first operands are read before the results leave.  Power is what bounds this kernel: every byte that does not move
-// is time.  75600 x 5120 -> 5120 855 us, 4.6 PFLOP/s, 32760 x 5120 -> 15360 1090 us, 4.7; 65520 x 1536 -> 8960 470 us, 3.8: there the results,
-// 1.2 GB, leave after every six steps, and the matrix pipe waits meanwhile.  The clock is 1.72 to 1.77 GHz in it, the pipe 65 % busy;
+// is time.  75600 x 5120 -> 5120 868 us, 4.6 PFLOP/s, 32760 x 5120 -> 15360 1097 us, 4.7; 65520 x 1536 -> 8960 471 us, 3.8: there the results,
+// 1.2 GB, leave after every six steps (413 us without their stores).  The clock is 1.72 to 1.77 GHz in it, the pipe 65 % busy;
 // of 736 us at 65536 x 5120 -> 5120, 620 are left without the copies, 584 without the LDS reads, 579 for the products alone.  (K of more
 // than one step.)
 using MxBig = MxTile<2, 2, 4, 4, 3>;
