@@ -562,8 +562,9 @@ void launch_layer_fwd(const LayerArgs& a, hipStream_t stream) {
   const int rows = min(a.rows, a.M);
   // Two rows at a time share the vectors (75600 x 5120 601 -> 541 us, 20000 x 8192 256 -> 232, 20000 x 13824 414 -> 404), where there are so many
   // that the chip is full all the same (1000 x 5120 11.5 / 12.2, 1000 x 1536 6.6 / 7.8); a wavefront's rows only on their way into codes, two of
-  // which are a line (65520 x 1536 -> 8960 612 -> 598; 65520 x 1536 by itself 141 / 143).
-  const bool two = rows > 1 && a.M >= 4096 && (a.codes || (a.K > 2048 && (a.gate.v || a.scale.v || a.shift.v)));
+  // which are a line (65520 x 1536 -> 8960 612 -> 598; 65520 x 1536 by itself 141 / 143).  (A grid has fewer than 2^32 threads: 2^22 rows of 1024
+  // would not fit.)
+  const bool two = rows > 1 && a.M >= 4096 && (a.codes || (a.K > 2048 && (a.gate.v || a.scale.v || a.shift.v)) || a.M > (1 << 21));
   const int per_sample = two ? (rows + 1) / 2 : rows, whole = a.M / rows, left = a.M - whole * rows;
   const int groups = whole * per_sample + (two ? (left + 1) / 2 : left);
 #define LAYER_FWD_(T, CH, ROWS, MX, NT) \

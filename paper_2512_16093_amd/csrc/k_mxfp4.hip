@@ -275,7 +275,7 @@ struct MxTile {
   static constexpr int COPIES = (XP + WP) / 2;                      // ... two at a time
   static constexpr int EX = M / 128, EW = N / 128;                  // pieces (128 rows, 1 KiB) of a step's exponents: one a wavefront
   static constexpr int STAGE = (M + N) * MX_REC, EXPS = (M + N) * 8;
-  static constexpr int SLOTS = STAGES > 4 ? 4 : 2, LDS = STAGES * STAGE + SLOTS * EXPS;   // (exponents of the steps under way)
+  static constexpr int LDS = STAGES * STAGE + 2 * EXPS;             // (exponents of two steps)
   static constexpr int TAIL = (STAGES + 1) / 2;                     // last steps, behind which less than the usual is copied
   static constexpr int EPI = 32 * CT * 2 + MX_EPI_PITCH;            // bytes of a staged output row
   // A wavefront's copies of halves `from` .. `to` (counted from a step's first) that are under way where `left` steps follow that one.
@@ -284,7 +284,7 @@ struct MxTile {
     for (int h = from; h <= to; ++h) n += h / 2 <= left ? XP + WP + (h % 2 == 0) : 0;
     return n;
   }
-  static_assert(WM * WN == 4 && M % 128 == 0 && N % 128 == 0 && M <= MX_TILE_ROWS && N <= MX_TILE_ROWS && EX + EW <= 4 && STAGES >= 3 && STAGES <= 8, "the copies' shares");
+  static_assert(WM * WN == 4 && M % 128 == 0 && N % 128 == 0 && M <= MX_TILE_ROWS && N <= MX_TILE_ROWS && EX + EW <= 4 && STAGES >= 3 && STAGES <= 4, "the copies' shares");
   static_assert(4 * 32 * EPI <= STAGES * STAGE && EPI % 16 == 0, "output staging fits the stages");
 };
 
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
     const unsigned to = lds0 + stage * T::STAGE;
     if (i < T::XP / 2) copy_pair(px + (size_t)h * RPx * MX_REC, lane16, to + T::XP * wv * 1024, i);
     else if (i < T::COPIES) copy_pair(pw + (size_t)h * RPw * MX_REC, lane16, to + T::M * MX_REC + T::WP * wv * 1024, i - T::XP / 2);
-    else copy_piece(pe + (h >> 1) * e_step, lane16, lds0 + STAGES * T::STAGE + ((h >> 1) % T::SLOTS) * T::EXPS + ep * 1024);
+    else copy_piece(pe + (h >> 1) * e_step, lane16, lds0 + STAGES * T::STAGE + ((h >> 1) & 1) * T::EXPS + ep * 1024);
   };
   auto copy_half = [&](int h, int stage) __attribute__((always_inline)) {
 #pragma unroll
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
     else wf[i - RT] = *(const v4i*)(s + T::M * MX_REC + (CT * wn + i - RT) * 32 * MX_REC);
   };
   auto read_exp = [&](int step, int i, uint32_t (&xs)[RT], uint32_t (&ws)[CT]) __attribute__((always_inline)) {
-    const unsigned char* s = lds + STAGES * T::STAGE + (step % T::SLOTS) * T::EXPS + 8 * l32 + 4 * hf;
+    const unsigned char* s = lds + STAGES * T::STAGE + (step & 1) * T::EXPS + 8 * l32 + 4 * hf;
     if (i < RT) xs[i] = *(const uint32_t*)(s + (RT * wm + i) * 256);
     else ws[i - RT] = *(const uint32_t*)(s + T::M * 8 + (CT * wn + i - RT) * 256);
   };
@@ -410,8 +410,6 @@ __global__ void __launch_bounds__(256, PER_CU) mxfp4_gemm_kernel(const uint8_t* 
       ++step;                             \
     }                                     \
   }
-  MX_LAST(3)
-  MX_LAST(2)
   MX_LAST(1)
   MX_LAST(0)
 #undef MX_LAST

@@ -30,11 +30,6 @@ __device__ __forceinline__ size_t mx_chunk_at(int RP, int row, int kb, int c) {
 }
 __device__ __forceinline__ size_t mx_exp_at(int RP, int row, int kb, int c) { return ((size_t)kb * RP + row) * 8 + 4 * (c & 1) + (c >> 1); }
 
-// The largest of a quad of lanes, in all four.
-__device__ __forceinline__ float quad_max(float x) {
-  x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xB1, 0xf, 0xf, true)));
-  return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4E, 0xf, 0xf, true)));
-}
 // The exponent's byte of a block whose largest magnitude is amax: floor(log2 amax) - 2, so that the quotients stay below 8, at
 // least -126 (the quotient's scale is then a normal number); 255 where amax is infinite or NaN.
 __device__ __forceinline__ uint32_t mx_exponent(float amax) {

@@ -219,3 +219,23 @@ def test_offsets_beyond_32_bits(M, K):
     g, M, x, v, y, h, at = _check_forward(1, M, K, "all")
     del x, y
     _check_backward(g, M, 1, h, v, at)
+
+
+def test_the_most_rows_of_the_widest_teams():
+    """2^22 rows of 1024 threads each would be 2^32 threads, more than a launch has."""
+    M, K = 1 << 22, 12296
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 4.2 * M * K:
+        pytest.skip("two tensors of 103 GB do not fit beside what is on the card")
+    x, y = (torch.zeros((M, K), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    few = _rand(_gen(1), (4, K), 2.0)
+    for at in (0, M // 2, M - 4):
+        x[at:at + 4] = few
+    bias = _rand(_gen(2), K)
+    sla.norm_layer_fwd(x, bias=bias, out=y)
+    want = sla.norm_layer_fwd(few, bias=bias)[0]
+    for at in (0, M // 2, M - 4):
+        assert torch.equal(y[at:at + 4], want)
+    assert torch.equal(y[M // 2 + 4], bias) and torch.equal(y[M - 5], bias)
+    del x, y
+    torch.cuda.empty_cache()

@@ -239,3 +239,41 @@ def test_a_block_of_these_operators_on_streams_and_in_graphs():
             torch.cuda.synchronize()
             replayed = [t.clone() for t in held]
             assert all(torch.equal(a, b) for a, b in zip(replayed, calls())), seed
+
+
+def test_calls_at_once_and_graphs_that_share_a_workspace():
+    """Two chains on two streams at the same time, each with workspaces of its own; two graphs captured over one workspace, replayed in
+    turn on one stream."""
+    K, N = 1536, 2056
+    r = np.random.default_rng(21)
+    wq = sla.mxfp4_quantize(_bf16(r, (N, K), 0.03).cuda())
+    xs = [_bf16(r, (M, K)).cuda() for M in (3000, 700)]
+    res = [_bf16(r, x.shape).cuda() for x in xs]
+    call = lambda i, ws=None: [*sla.mxfp4_norm_linear_fwd(xs[i], wq, N, res=res[i], workspace=ws), *sla.norm_layer_bwd(xs[i], res[i], dh=xs[i])[:1]]
+    alone = [[t.clone() for t in call(i)] for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    at_once = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                at_once[i].append(call(i))
+    for s in streams:
+        torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for got in at_once[i] for a, b in zip(got, alone[i]))
+    shared = torch.full((sla.mxfp4_bytes(3000, K),), 0xFF, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            graphs.append((g, call(i, shared)))
+    for i in (0, 1, 1, 0, 1, 0):
+        for t in graphs[i][1]:
+            t.zero_()
+        shared.fill_(0xFF)
+        graphs[i][0].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(graphs[i][1], alone[i])), i
