@@ -976,14 +976,15 @@ def norm_layer_fwd(x, w=None, bias=None, res=None, gate=None, scale=None, shift=
     M, K, device, h, args = _layer_args(x, w, bias, res, gate, scale, shift, h)
     if out is None:
         out = torch.empty_like(x)
+        at = out.data_ptr()
     else:
-        _of(out, "out", (M, K), device)
-    _go("norm_layer_fwd", device, *args, out.data_ptr(), M, K, eps)
+        at = _of(out, "out", (M, K), device)
+    _go("norm_layer_fwd", device, *args, at, M, K, eps)
     return out, h
 
 
 def norm_layer_bwd_workspace_bytes(M, K, rows):
-    return lib().norm_layer_bwd_workspace_bytes(M, K, rows)
+    return (_lib or lib()).norm_layer_bwd_workspace_bytes(M, K, rows)
 
 
 def norm_layer_bwd(dy, h, w=None, bias=None, dh=None, res=None, gate=None, scale=None, shift=None, eps=1e-6, dx=None, dres=None,
@@ -1000,19 +1001,38 @@ def norm_layer_bwd(dy, h, w=None, bias=None, dh=None, res=None, gate=None, scale
         raise ValueError("the gate's gradient needs res")
     at = (dy.data_ptr(), _maybe(dh, "dh", one, device), _of(h, "h", one, device), _maybe(res, "res", one, device),
           _maybe(w, "w", (K,), device), _maybe(bias, "bias", (K,), device), _by_ref(mod))
-    dx = torch.empty_like(dy) if dx is None else dx
-    _of(dx, "dx", one, device)
+    if dx is None:
+        dx = torch.empty_like(dy)
+        dx_at = dx.data_ptr()
+    else:
+        dx_at = _of(dx, "dx", one, device)
+    dres_at = None
     if gate is not None:
-        dres = torch.empty_like(dy) if dres is None else dres
-        _of(dres, "dres", one, device)
-    new = lambda t, *shape: torch.empty(shape, dtype=torch.float32, device=dy.device) if want_vectors and t is not None else None
-    dw, db, dgate, dscale, dshift = new(w, K), new(bias, K), new(gate, S, K), new(scale, S, K), new(shift, S, K)
-    grads, ws, ws_bytes = None, None, 0
-    if any(t is not None for t in (dw, db, dgate, dscale, dshift)):
-        grads = NormLayerGrads(_at(dw), _at(db), _at(dgate), _at(dscale), _at(dshift))
-        workspace = _scratch(workspace, norm_layer_bwd_workspace_bytes(M, K, M // S), dy.device, "norm_layer_bwd")
-        ws, ws_bytes = _bytes_on(workspace, "workspace", device), workspace.numel()
-    _go("norm_layer_bwd", device, *at, dx.data_ptr(), _at(dres), _by_ref(grads), M, K, eps, ws, ws_bytes)
+        if dres is None:
+            dres = torch.empty_like(dy)
+            dres_at = dres.data_ptr()
+        else:
+            dres_at = _of(dres, "dres", one, device)
+    dw = db = dgate = dscale = dshift = grads = ws = None
+    ws_bytes = 0
+    if want_vectors:
+        f32 = torch.float32
+        dw = None if w is None else w.new_empty(K, dtype=f32)
+        db = None if bias is None else bias.new_empty(K, dtype=f32)
+        dgate = None if gate is None else gate.new_empty((S, K))
+        dscale = None if scale is None else scale.new_empty((S, K))
+        dshift = None if shift is None else shift.new_empty((S, K))
+        if dw is not None or db is not None or mod is not None:
+            grads = NormLayerGrads(_at(dw), _at(db), _at(dgate), _at(dscale), _at(dshift))
+            if workspace is None:
+                ws_bytes = norm_layer_bwd_workspace_bytes(M, K, M // S)
+                if ws_bytes == 0:
+                    raise ValueError("unsupported problem for norm_layer_bwd")
+                workspace = dy.new_empty(ws_bytes, dtype=torch.uint8)
+                ws = workspace.data_ptr()
+            else:
+                ws, ws_bytes = _bytes_on(workspace, "workspace", device), workspace.numel()
+    _go("norm_layer_bwd", device, *at, dx_at, dres_at, _by_ref(grads), M, K, eps, ws, ws_bytes)
     return LayerGrads(dx, dres, dw, db, dgate, dscale, dshift)
 
 
