@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(64 * KSPLIT) mxfp4_gemm_split_kernel(const uin
 // A half's first 64 features are read while the second ones of the half before are multiplied; in the middle of a half, when all
 // of its operands are in registers, the workgroup meets: behind that its stage is free for the half STAGES on, and the next half's
 // has arrived.
-// With one or two wavefronts a SIMD the products alone set the time, and what stands before and behind them: 512 x 5120 -> 13824 22.2 us
+// With one or two wavefronts a SIMD the products alone set the time, and what stands before and behind them: 512 x 5120 -> 13824 21.9 us
 // with tiles of 256 x 128, without copies 18.6, without LDS reads too 17.2; 4096 x 5120 -> 5120 55 us, 3.9 PFLOP/s.
 // ---------------------------------------------------------------------------
 constexpr int MX_EPI_PITCH = 16;                  // bytes behind each staged output row
@@ -697,6 +697,9 @@ static void launch_split(const uint8_t* x, const uint8_t* xe, const uint8_t* w, 
 //   walk from 1024 of its tiles and four steps on: 16384 x 5120 -> 5120 (1280) walk 191, wide 200, 20000 x 1536 -> 8960 (2765) 156 / 158; 12000 x
 //   1536 -> 4608 (846) 59.6 / 48.1, 8192 x 5120 -> 5120 (640) 119 / 113, 65536 x 640 -> 1280 (1280) 47.9 / 46.5;
 //   at least 512 wide tiles: 4096 x 5120 -> 5120 (640) wide 54.9, square 57.1, walk 65; 2048 x 5120 -> 5120 (320) 33.2 / 31.8 / 32.4;
+//   fewer where they leave a compute unit no more to do than square ones, half their size, and the contraction is long: 1024 x 5120 -> 13824
+//   (432 wide, 864 square) 37.0 / 41.6, 1024 x 8960 -> 5120 (160, 320) 28.1 / 31.1, 512 x 5120 -> 13824 (216, 432) 21.9 / 22.6, 512 x 2560 -> 13824
+//   12.9 / 13.1; but 1024 x 2048 -> 8192 (256, 512) 12.1 / 10.9; 1800 x 5120 -> 5120 (320, 600) 32.6 / 30.6, 700 x 13824 -> 5120 (120, 240) 39.5 / 30.6;
 //   square from 64 tiles on: 1024 x 1536 -> 1536 (96) square 6.0, split 6.9; 256 x 5120 -> 5120 (80) 11.9 / 14.1; 300 x 2560 -> 2560 (60) 7.4 /
 //   6.2; 128 x 5120 -> 5120 (40) 11.4 / 8.7; with four stages up to 256 tiles: 512 x 5120 -> 5120 (160) 12.7 against 13.5, 700 x 8960 -> 1536
 //   (72) 18.4 / 20.6, but 1024 x 5120 -> 5120 (320) 22.1 / 20.9;
@@ -714,7 +717,8 @@ void launch_mxfp4_gemm(const uint8_t* x, const uint8_t* xe, const uint8_t* w, co
     if (K > 16 * MX_STEP) return launch_split<1, 1, 8>(MX_ARGS);
     return launch_split<1, 1, 4>(MX_ARGS);
   }
-  if (tiles(256, 128) >= 512) return launch_tiles<4, 1, 2, 4, 3, 2>(MX_ARGS);
+  auto rounds = [&](int m, int n) { return (tiles(m, n) + 255) / 256; };   // tiles of a compute unit
+  if (tiles(256, 128) >= 512 || (K > 8 * MX_STEP && 2 * rounds(256, 128) <= rounds(128, 128))) return launch_tiles<4, 1, 2, 4, 3, 2>(MX_ARGS);
   if (tiles(128, 128) > 256) return launch_tiles<2, 2, 2, 2, 3, 3>(MX_ARGS);
   if (tiles(128, 128) >= 64) return launch_tiles<2, 2, 2, 2, 4, 2>(MX_ARGS);
   launch_split<2, 2, 4>(MX_ARGS);

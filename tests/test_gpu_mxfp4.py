@@ -241,6 +241,12 @@ def test_a_block_of_these_operators_on_streams_and_in_graphs():
             assert all(torch.equal(a, b) for a, b in zip(replayed, calls())), seed
 
 
+@pytest.mark.parametrize("M,N,K", [(512, 13824, 2312), (1023, 5128, 2056), (300, 13832, 4096), (1800, 5120, 2304), (700, 5120, 2560)])
+def test_wide_tiles_that_are_few(M, N, K):
+    """Contractions of more than 2048 features in one and two rounds of wide tiles, and beside them calls that keep the square ones."""
+    test_linear(M, N, K)
+
+
 def test_calls_at_once_and_graphs_that_share_a_workspace():
     """Two chains on two streams at the same time, each with workspaces of its own; two graphs captured over one workspace, replayed in
     turn on one stream."""
