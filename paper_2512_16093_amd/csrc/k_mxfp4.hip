@@ -696,10 +696,11 @@ static void launch_split(const uint8_t* x, const uint8_t* xe, const uint8_t* w, 
 // 128 with 3 or 4 stages, three or two to a compute unit; split: RT, CT, wavefronts):
 //   walk from 1024 of its tiles and four steps on: 16384 x 5120 -> 5120 (1280) walk 191, wide 200, 20000 x 1536 -> 8960 (2765) 156 / 158; 12000 x
 //   1536 -> 4608 (846) 59.6 / 48.1, 8192 x 5120 -> 5120 (640) 119 / 113, 65536 x 640 -> 1280 (1280) 47.9 / 46.5;
-//   at least 512 wide tiles: 4096 x 5120 -> 5120 (640) wide 54.9, square 57.1, walk 65; 2048 x 5120 -> 5120 (320) 33.2 / 31.8 / 32.4;
-//   fewer where they leave a compute unit no more to do than square ones, half their size, and the contraction is long: 1024 x 5120 -> 13824
-//   (432 wide, 864 square) 37.0 / 41.6, 1024 x 8960 -> 5120 (160, 320) 28.1 / 31.1, 512 x 5120 -> 13824 (216, 432) 21.9 / 22.6, 512 x 2560 -> 13824
-//   12.9 / 13.1; but 1024 x 2048 -> 8192 (256, 512) 12.1 / 10.9; 1800 x 5120 -> 5120 (320, 600) 32.6 / 30.6, 700 x 13824 -> 5120 (120, 240) 39.5 / 30.6;
+//   wide from 512 of its tiles on: 4096 x 5120 -> 5120 (640) wide 54.9, square 57.1, walk 65; 2048 x 5120 -> 5120 (320) 33.2 / 31.8 / 32.4;
+//   fewer of the larger tiles where the contraction is long and the busiest compute unit has no more to do with them: walk 5000 x 13824 -> 5120
+//   (400) 168, wide (800) 181, 2048 x 5120 -> 13824 (432) 71.1 / 74.5, 4096 x 5120 -> 15360 (960) 147 / 152, but 2000 x 2560 -> 15360 (480) 44.6 / 43.6
+//   and 8192 x 8960 -> 5120 (640, 3 rounds to 5) 167 / 164; wide 1024 x 5120 -> 13824 (432) 37.0, square (864) 41.6, 1024 x 8960 -> 5120 (160) 28.1 /
+//   31.1, 512 x 2560 -> 13824 (216) 12.9 / 13.1, but 1024 x 2048 -> 8192 (256) 12.1 / 10.9, 1800 x 5120 -> 5120 (320 to 600, 2 rounds to 3) 32.6 / 30.6;
 //   square from 64 tiles on: 1024 x 1536 -> 1536 (96) square 6.0, split 6.9; 256 x 5120 -> 5120 (80) 11.9 / 14.1; 300 x 2560 -> 2560 (60) 7.4 /
 //   6.2; 128 x 5120 -> 5120 (40) 11.4 / 8.7; with four stages up to 256 tiles: 512 x 5120 -> 5120 (160) 12.7 against 13.5, 700 x 8960 -> 1536
 //   (72) 18.4 / 20.6, but 1024 x 5120 -> 5120 (320) 22.1 / 20.9;
@@ -707,7 +708,12 @@ static void launch_split(const uint8_t* x, const uint8_t* xe, const uint8_t* w, 
 void launch_mxfp4_gemm(const uint8_t* x, const uint8_t* xe, const uint8_t* w, const uint8_t* we, const void* bias, void* y, int M,
                        int N, int K, hipStream_t stream) {
   auto tiles = [&](int m, int n) { return (long long)((M + m - 1) / m) * ((N + n - 1) / n); };
-  if (K > 3 * MX_STEP && tiles(256, 256) >= 1024) {      // (256 workgroups: one to a compute unit, a multiple of the 8 XCDs)
+  // what the busiest compute unit has to do, in square tiles
+  auto load = [&](int m, int n) { return m * n / 16384 * ((tiles(m, n) + 255) / 256); };
+  const bool deep = K > 8 * MX_STEP;
+  if ((K > 3 * MX_STEP && tiles(256, 256) >= 1024) ||
+      (deep && load(256, 256) <= load(256, 128) && 6 * load(256, 256) <= 7 * load(128, 128))) {
+    // (256 workgroups: one to a compute unit, a multiple of the 8 XCDs)
     mxfp4_gemm_walk_kernel<<<256, 256, 0, stream>>>(x, xe, w, we, (const bf16_t*)bias, (bf16_t*)y, M, N, mx_steps(K), (M + 255) / 256, (N + 255) / 256);
     return;
   }
@@ -717,8 +723,7 @@ void launch_mxfp4_gemm(const uint8_t* x, const uint8_t* xe, const uint8_t* w, co
     if (K > 16 * MX_STEP) return launch_split<1, 1, 8>(MX_ARGS);
     return launch_split<1, 1, 4>(MX_ARGS);
   }
-  auto rounds = [&](int m, int n) { return (tiles(m, n) + 255) / 256; };   // tiles of a compute unit
-  if (tiles(256, 128) >= 512 || (K > 8 * MX_STEP && 2 * rounds(256, 128) <= rounds(128, 128))) return launch_tiles<4, 1, 2, 4, 3, 2>(MX_ARGS);
+  if (tiles(256, 128) >= 512 || (deep && load(256, 128) <= load(128, 128))) return launch_tiles<4, 1, 2, 4, 3, 2>(MX_ARGS);
   if (tiles(128, 128) > 256) return launch_tiles<2, 2, 2, 2, 3, 3>(MX_ARGS);
   if (tiles(128, 128) >= 64) return launch_tiles<2, 2, 2, 2, 4, 2>(MX_ARGS);
   launch_split<2, 2, 4>(MX_ARGS);

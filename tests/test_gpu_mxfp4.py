@@ -241,9 +241,9 @@ def test_a_block_of_these_operators_on_streams_and_in_graphs():
             assert all(torch.equal(a, b) for a, b in zip(replayed, calls())), seed
 
 
-@pytest.mark.parametrize("M,N,K", [(512, 13824, 2312), (1023, 5128, 2056), (300, 13832, 4096), (1800, 5120, 2304), (700, 5120, 2560)])
-def test_wide_tiles_that_are_few(M, N, K):
-    """Contractions of more than 2048 features in one and two rounds of wide tiles, and beside them calls that keep the square ones."""
+@pytest.mark.parametrize("M,N,K", [(512, 13824, 2312), (1023, 5128, 2056), (300, 13832, 4096), (1800, 5120, 2304), (700, 5120, 2560), (1024, 15360, 2312), (2040, 13824, 2056), (5000, 5128, 2056)])
+def test_large_tiles_that_are_few(M, N, K):
+    """Contractions of more than 2048 features in one and two rounds of wide or walked tiles, and calls that keep the square ones."""
     test_linear(M, N, K)
 
 
