@@ -243,7 +243,7 @@ __device__ __forceinline__ void copy_pair(const char* base, unsigned off, unsign
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0\n\tglobal_load_lds_dwordx4 %1, %0 offset:1024"
                  : : "s"(base), "v"(off), "s"(lds_addr) : "memory", "m0");
   else
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0 offset:2048\n\tglobal_load_lds_dwordx4 %1, %0 offset:3072"
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0 offset:0x800\n\tglobal_load_lds_dwordx4 %1, %0 offset:0xc00"
                  : : "s"(base), "v"(off), "s"(lds_addr) : "memory", "m0");
 }
 
