@@ -937,19 +937,20 @@ def _modulation(M, K, device, gate, scale, shift):
     S, at = 0, []
     for t, what in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
         if t is None:
-            at += [(None, 0)]
+            at += (None, 0)
             continue
-        if t.dtype is not torch.float32 or t.dim() != 2 or t.shape[1] != K or t.stride(1) != 1 or t.get_device() != device:
+        shape, stride = t.shape, t.stride()
+        if t.dtype is not torch.float32 or len(shape) != 2 or shape[1] != K or stride[1] != 1 or t.get_device() != device:
             raise ValueError("%s: expected a float32 tensor [samples, %d] with contiguous features on the CUDA device of the other "
                              "tensors" % (what, K))
-        n = t.shape[0]
-        if n < 1 or M % n or (S and n != S):
+        n = shape[0]
+        if n < 1 or (n != S and (S or M % n)):
             raise ValueError("gate, scale and shift: one number of samples, of M / samples rows each")
         S = n
-        at += [(t.data_ptr(), t.stride(0) if n > 1 else 0)]         # (of one sample the stride says nothing)
+        at += (t.data_ptr(), stride[0] if n > 1 else 0)             # (of one sample the stride says nothing)
     if S == 0:
         return None, 1
-    (g, gs), (c, cs), (h, hs) = at
+    g, gs, c, cs, h, hs = at
     return NormModulation(g, c, h, gs, cs, hs, M // S), S
 
 

@@ -213,3 +213,15 @@ def test_streams_and_captured_graphs():
         torch.cuda.synchronize()
         replayed = [t.clone() for t in held]
         assert all(torch.equal(a, b) for a, b in zip(replayed, calls())), seed
+
+
+def test_numbers_of_samples_that_do_not_fit_are_refused():
+    x, v = torch.zeros((6, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((6, 64), device="cuda")
+    for bad in (v[:0], v[:4], torch.zeros((12, 64), device="cuda")):
+        for kw in (dict(scale=bad), dict(shift=bad), dict(scale=v[:2], shift=bad), dict(scale=bad, shift=v[:2])):
+            with pytest.raises(ValueError):
+                sla.norm_layer_fwd(x, **kw)
+            with pytest.raises(ValueError):
+                sla.norm_layer_bwd(x, x, **kw)
+    with pytest.raises(ValueError):
+        sla.norm_layer_fwd(x, scale=v[:2], shift=v[:3])
