@@ -2,9 +2,16 @@
 // (include/mxfp4.h) as well.
 //
 // A team of T threads per row, as in k_norm.hip: the row stays in registers between its sums and its result, so every tensor
-// is read or written once: bound by HBM (a copy reaches 4.9 TB/s, an addition of two tensors 5.8).  Mean first, then the sum of the
-// squared deviations from it: two passes over registers, no difference of large squares.  All in fp32; the stored stream is rounded to bf16
-// before it is normed, because its readers find it so, the result once.
+// is read or written once: bound by HBM (a copy reaches 4.9 TB/s, an addition of two tensors 5.8).  All in fp32; the stored stream is rounded to
+// bf16 before it is normed, because its readers find it so, the result once.
+// Two passes over registers: the sum S of the row, of which row_mean makes p, the bf16 number next to the mean, and c = (S - K p) / K, the rest of
+// it; then the sum of (x - p)^2.  The deviations are (x - p) - c, the variance mean((x - p)^2) - c^2.  So the rounding of the mean is in no
+// deviation (deviations from the rounded mean put 0.7 % on the n of 999 equal features beside one that is a bf16 step larger, and the n of
+// constant rows up to 1): differences of bf16 numbers are exact, or off by 2^-24 of themselves, and those of a constant row zero, c too.  S is
+// exact in fp32 where a row's features are within a factor of four (at most 2^14 numbers of 10 bits), and else its rounding is small against the
+// deviations (n off by 2^-18 at most in 2400 rows with features of any other size among equal ones).  Nor do the squares cancel: no x lies
+// between the bf16 numbers a < b around the mean, so (x - a)(x - b) >= 0 and the variance is at least (mean - a)(b - mean), which is at least
+// c^2, p being the nearer of the two.
 // Measured: forward with gate and modulation 75600 x 5120 541 us, 5.7 TB/s, 32760 x 5120 239, 65520 x 1536 145 (5.5), 20000 x 13824 404, without
 // residual 75600 x 5120 280 (5.5); into codes 75600 x 5120 456 (5.5), 65520 x 1536 115; one row of 5120 2.9.  Backward with everything
 // 65520 x 1536 252 us, 4.8 TB/s, 32760 x 5120 419 (4.8), 8192 x 5120 116, 129 x 1536 12.
@@ -22,6 +29,17 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
 // Share e of a row: its address is the row's, the same for a wavefront, and 32 bits of each lane's.
 __device__ __forceinline__ const bf16_t* share_of(const bf16_t* row, int e) { return (const bf16_t*)((const char*)row + 16u * (unsigned)e); }
 __device__ __forceinline__ bf16_t* share_of(bf16_t* row, int e) { return (bf16_t*)((char*)row + 16u * (unsigned)e); }
+
+// p and c of a row whose K features have the sum s.
+struct RowMean { float p, c; };
+__device__ __forceinline__ RowMean row_mean(float s, float K, float inv) {
+  const float p = bf16_lo(pack_bf16x2(s * inv, 0.f));
+  return {p, __builtin_fmaf(-K, p, s) * inv};
+}
+// 1 / sqrt(variance + eps), given mean((x - p)^2) and c.  (Rounded, the variance could fall below zero.)
+__device__ __forceinline__ float row_factor(float square, float c, float eps) {
+  return __builtin_amdgcn_rsqf(__builtin_fmaxf(__builtin_fmaf(-c, c, square), 0.f) + eps);
+}
 
 // MX: codes instead of y.  A team takes ROWS rows of one sample at a time: two share what they read of the vectors, which come from the
 // caches, 12 bytes a feature with a gate, scale and shift.
@@ -96,7 +114,7 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs 
 #pragma unroll
     for (int c = 0; c < CH; ++c) gate(c);
   }
-  float mean[ROWS] = {}, rs[ROWS] = {};
+  float sum[ROWS] = {}, rs[ROWS] = {};
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int e = t + c * T;
@@ -120,16 +138,21 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs 
         unpack8(v[r][c], x);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) mean[r] += x[i];
+      for (int i = 0; i < 8; ++i) sum[r] += x[i];
     }
   }
   if constexpr (EARLY) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) vectors(c);
   }
-  sums(mean, red[0]);
+  sums(sum, red[0]);
+  RowMean mean[ROWS];
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) mean[r] *= inv;
+  for (int r = 0; r < ROWS; ++r) {
+    mean[r] = row_mean(sum[r], (float)a.K, inv);
+    // (a scalar: with two rows a wavefront it decides over one more per SIMD.  65520 x 1536 into codes 129 -> 125 us)
+    if constexpr (T == 64) mean[r].p = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(mean[r].p)));
+  }
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     if (t + c * T >= n) break;
@@ -138,12 +161,15 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs 
       float x[8];
       unpack8(v[r][c], x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) rs[r] = __builtin_fmaf(x[i] - mean[r], x[i] - mean[r], rs[r]);
+      for (int i = 0; i < 8; ++i) rs[r] = __builtin_fmaf(x[i] - mean[r].p, x[i] - mean[r].p, rs[r]);
     }
   }
   sums(rs, red[1]);
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) rs[r] = __builtin_amdgcn_rsqf(rs[r] * inv + a.eps);
+  for (int r = 0; r < ROWS; ++r) {
+    rs[r] = row_factor(rs[r] * inv, mean[r].c, a.eps);
+    mean[r].c *= -rs[r];                         // (n = (x - p) rs - c rs)
+  }
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int e = t + c * T;
@@ -155,7 +181,7 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs 
         float x[8], u[8];
         unpack8(v[r][c], x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean[r]) * rs[r];
+        for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i] - mean[r].p, rs[r], mean[r].c);
         if (a.w) {
           unpack8(w[c], u);
 #pragma unroll
@@ -257,7 +283,7 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += x[i];
     }
-    const float mean = team_sum<T>(sum, red) * inv;
+    const RowMean mean = row_mean(team_sum<T>(sum, red), (float)a.K, inv);
     auto unpack4 = [](uint32_t lo, uint32_t hi, float (&v)[4]) __attribute__((always_inline)) {
       v[0] = bf16_lo(lo); v[1] = bf16_hi(lo); v[2] = bf16_lo(hi); v[3] = bf16_hi(hi);
     };
@@ -265,7 +291,7 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
       const float4 x = from[q * T * CH + t + c * T];
       v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
     };
-    // of half a share: h - mean, dy, and g = dy o (1 + scale) o w
+    // of half a share: h - p, dy, and g = dy o (1 + scale) o w
     auto half = [&](int c, int q, float (&x)[4], float (&y)[4], float (&g)[4]) __attribute__((always_inline)) {
       float u[4];
       held(up, c, q, u);
@@ -281,7 +307,7 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[i] -= mean;
+        x[i] -= mean.p;
         g[i] = y[i] * u[i];
       }
     };
@@ -311,8 +337,8 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
 #pragma unroll
       for (int i = 0; i < T / 64; ++i) { ss += red3[0][i]; sg += red3[1][i]; xg += red3[2][i]; }
     }
-    // (dx = dh + r (g - mean(g) - x r^2 mean(x g)): r^2 mean(x g) as two products, r is up to 1 / sqrt(eps))
-    const float r = __builtin_amdgcn_rsqf(ss * inv + a.eps), dot = xg * inv * r * r, mg = sg * inv;
+    // dx = dh + r (g - mean(g) - n mean(n g)), n = (h - p) r - c r
+    const float mg = sg * inv, r = row_factor(ss * inv, mean.c, a.eps), off = -mean.c * r, dot = __builtin_fmaf(-mean.c, mg, xg * inv) * r;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int e = t + c * T;
@@ -324,8 +350,9 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_bwd_kernel(LayerBwdAr
         half(c, q, x, y, g);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+          x[i] = __builtin_fmaf(x[i], r, off);
           a0[c][4 * q + i] += y[i];
-          a1[c][4 * q + i] = __builtin_fmaf(y[i], x[i] * r, a1[c][4 * q + i]);
+          a1[c][4 * q + i] = __builtin_fmaf(y[i], x[i], a1[c][4 * q + i]);
         }
         unpack4(q ? rh[c].z : rh[c].x, q ? rh[c].w : rh[c].y, d);
 #pragma unroll
