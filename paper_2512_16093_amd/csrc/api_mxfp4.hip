@@ -96,6 +96,7 @@ int mxfp4_linear_fwd(const void* x, const void* wq, size_t wq_bytes, const void*
   if (launch_mxfp4_linear_few(x, (const uint8_t*)wq, exps_of(wq, N, K), bias, y, M, N, K, (hipStream_t)stream)) return launch_status();
   uint8_t *codes = (uint8_t*)workspace, *exps = exps_of(workspace, M, K);
   launch_mxfp4_quantize(x, M, K, codes, exps, (hipStream_t)stream);
+  if (int st = launch_status()) return st;
   launch_mxfp4_gemm(codes, exps, (const uint8_t*)wq, exps_of(wq, N, K), bias, y, M, N, K, (hipStream_t)stream);
   return launch_status();
 }
@@ -124,6 +125,7 @@ int mxfp4_norm_linear_fwd(const void* x, const void* res, const void* norm_w, co
   a.codes = (uint8_t*)workspace;
   a.exps = exps_of(workspace, M, K);
   launch_layer_fwd(a, (hipStream_t)stream);
+  if (int st = launch_status()) return st;
   launch_mxfp4_gemm(a.codes, a.exps, (const uint8_t*)wq, exps_of(wq, N, K), bias, y, M, N, K, (hipStream_t)stream);
   return launch_status();
 }

@@ -48,13 +48,17 @@ __global__ void __launch_bounds__(T == 64 ? 256 : T) layer_fwd_kernel(LayerArgs 
   __shared__ float red[2][ROWS][T / 64];
   constexpr int TEAMS = T == 64 ? 4 : 1;
   const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = a.K / 8;
-  int block = blockIdx.x;
+  int block = blockIdx.x, blocks = gridDim.x;
+  if constexpr (T == 1024) {                   // (of a grid of two rows, see launch_layer_fwd)
+    block += blockIdx.y * blocks;
+    blocks *= gridDim.y;
+  }
   if constexpr (MX) {
     // Workgroups are dealt round-robin over the 8 XCDs: of every 8 RUN, RUN neighbours to each, so that the 16 rows whose exponents
     // share a line are one L2's.
     constexpr int RUN = 16 / (ROWS * TEAMS);
     const int from = block / (8 * RUN) * (8 * RUN);
-    if (from + 8 * RUN <= (int)gridDim.x) block = from + ((block - from) & 7) * RUN + ((block - from) >> 3);
+    if (from + 8 * RUN <= blocks) block = from + ((block - from) & 7) * RUN + ((block - from) >> 3);
   }
   const int group = TEAMS * block + (T == 64 ? wave : 0);
   if (group >= groups) return;                 // (T > 64: the whole workgroup)
@@ -589,13 +593,18 @@ void launch_layer_fwd(const LayerArgs& a, hipStream_t stream) {
   const int rows = min(a.rows, a.M);
   // Two rows at a time share the vectors (75600 x 5120 601 -> 541 us, 20000 x 8192 256 -> 232, 20000 x 13824 414 -> 404), where there are so many
   // that the chip is full all the same (1000 x 5120 11.5 / 12.2, 1000 x 1536 6.6 / 7.8); a wavefront's rows only on their way into codes, two of
-  // which are a line (65520 x 1536 -> 8960 612 -> 598; 65520 x 1536 by itself 141 / 143).  (A grid has fewer than 2^32 threads: 2^22 rows of 1024
-  // would not fit.)
+  // which are a line (65520 x 1536 -> 8960 612 -> 598; 65520 x 1536 by itself 141 / 143), and millions of any rows (2500000 x 520 1073 -> 1048,
+  // 2500000 x 5120 8810 -> 8660).
   const bool two = rows > 1 && a.M >= 4096 && (a.codes || (a.K > 2048 && (a.gate.v || a.scale.v || a.shift.v)) || a.M > (1 << 21));
   const int per_sample = two ? (rows + 1) / 2 : rows, whole = a.M / rows, left = a.M - whole * rows;
   const int groups = whole * per_sample + (two ? (left + 1) / 2 : left);
+  // A row of a grid has fewer than 2^32 threads: 2^22 teams of 1024 take two.
+  auto grid = [&](int T) {
+    const unsigned n = (unsigned)(T == 64 ? (groups + 3) / 4 : groups);
+    return (unsigned long long)n * T >> 32 ? dim3((n + 1) / 2, 2) : dim3(n);
+  };
 #define LAYER_FWD_(T, CH, ROWS, MX, NT) \
-  layer_fwd_kernel<T, CH, ROWS, MX, NT><<<(unsigned)(T == 64 ? (groups + 3) / 4 : groups), T == 64 ? 256 : T, 0, stream>>>(a, groups, per_sample)
+  layer_fwd_kernel<T, CH, ROWS, MX, NT><<<grid(T), T == 64 ? 256 : T, 0, stream>>>(a, groups, per_sample)
 #define LAYER_FWD(T, CH)                                                                                       \
   do {                                                                                                         \
     if (a.codes) {                                                                                             \

@@ -113,3 +113,38 @@ def test_nearly_constant_rows(K):
         # (the two products' own roundings are a few 2^-23 of their sizes, and the mean of g n is 54 additions deep: 2^-18 of its terms' sizes)
         fp32 = f * (N * (m + mean(m)) + off * mean(m * a) + a * mean(m * off) + 2.0 ** -15 * a * mean(m * a))
         assert (np.abs(_np(got.dx) - want) <= HALF * np.abs(want) + fp32).all()
+
+
+def test_the_most_rows_with_a_vector_each():
+    """2^22 rows in as many samples (of one vector, at stride 0) by the widest teams: 2^32 threads, more than a launch has in a row."""
+    M, K = 1 << 22, 12296
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 4.2 * M * K:
+        pytest.skip("two tensors of 103 GB do not fit beside what is on the card")
+    r = np.random.default_rng(3)
+    x = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda")
+    few, places = _cuda(2 * r.standard_normal((4, K))), (0, M // 2 - 2, M - 4)
+    for at in places:
+        x[at:at + 4] = few
+    v = {k: torch.from_numpy(r.standard_normal((1, K)).astype(np.float32)).cuda() for k in ("scale", "shift")}
+    wide = {k: t.expand(M, K) for k, t in v.items()}
+    want, rest = sla.norm_layer_fwd(few, **v)[0], v["shift"].bfloat16()[0]
+    q, _ = sla.mxfp4_norm_quantize(x, **wide)
+    codes, exps = sla.mxfp4_unpack(q, M, K)
+    del q
+    want_codes, want_exps = sla.mxfp4_unpack(sla.mxfp4_quantize(want), 4, K)
+    rest_codes, rest_exps = sla.mxfp4_unpack(sla.mxfp4_quantize(rest[None]), 1, K)
+    for at in places:
+        assert torch.equal(codes[at:at + 4], want_codes) and torch.equal(exps[at:at + 4], want_exps)
+    for at in (4, M // 2 + 2, M - 5):
+        assert torch.equal(codes[at], rest_codes[0]) and torch.equal(exps[at], rest_exps[0])
+    del codes, exps
+    torch.cuda.empty_cache()
+    y = torch.zeros_like(x)
+    sla.norm_layer_fwd(x, **wide, out=y)
+    for at in places:
+        assert torch.equal(y[at:at + 4], want)
+    for at in (4, M // 2 + 2, M - 5):
+        assert torch.equal(y[at], rest)
+    del x, y
+    torch.cuda.empty_cache()
