@@ -653,22 +653,22 @@ void launch_layer_bwd(const LayerBwdArgs& a, hipStream_t stream) {
   float *s0 = sums ? (float*)ws : nullptr, *s1 = sums ? (float*)(ws + one) : nullptr, *s2 = g.gate ? (float*)(ws + 2 * one) : nullptr;
   const unsigned grid = (unsigned)d.samples * d.chunks;
   const bool gate = a.gate.v != nullptr, nt = streams(a.M, a.K, 3 + (a.dh != nullptr) + 2 * gate);
-#define LAYER_BWD(T, CH)                                                                                            \
-  do {                                                                                                              \
-    constexpr int threads = T == 64 ? 256 : T;                                                                      \
-    if constexpr (T == 768) {   /* (never with a gate: there three shares do not fit the registers) */               \
-      if (nt) layer_bwd_kernel<T, CH, false, true><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);   \
-      else layer_bwd_kernel<T, CH, false, false><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);     \
-    } else if (gate) {                                                                                              \
-      if (nt) layer_bwd_kernel<T, CH, true, true><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);    \
-      else layer_bwd_kernel<T, CH, true, false><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);      \
-    } else {                                                                                                        \
-      if (nt) layer_bwd_kernel<T, CH, false, true><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);   \
-      else layer_bwd_kernel<T, CH, false, false><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);     \
-    }                                                                                                               \
+#define LAYER_BWD_(T, CH, GATE)                                                                                              \
+  do {                                                                                                                       \
+    constexpr int threads = T == 64 ? 256 : T;                                                                               \
+    if (nt) layer_bwd_kernel<T, CH, GATE, true><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);               \
+    else layer_bwd_kernel<T, CH, GATE, false><<<grid, threads, 0, stream>>>(a, d.chunks, d.per, s0, s1, s2);                 \
+  } while (0)
+#define LAYER_BWD(T, CH)                                                                                                     \
+  do {   /* (the widest rows have teams of their own with a gate and without) */                                             \
+    if constexpr (T == 512 && CH == 4) LAYER_BWD_(T, CH, true);                                                              \
+    else if constexpr (T == 768) LAYER_BWD_(T, CH, false);                                                                   \
+    else if (gate) LAYER_BWD_(T, CH, true);                                                                                  \
+    else LAYER_BWD_(T, CH, false);                                                                                           \
   } while (0)
   LAYER_BWD_TEAMS(a.K / 8, LAYER_BWD);
 #undef LAYER_BWD
+#undef LAYER_BWD_
   if (!sums && !g.gate) return;
   float *pw = g.w, *pb = g.b;
   if (d.parts > 1) {
