@@ -127,10 +127,16 @@ __device__ __forceinline__ uint4 t_op_swz(const unsigned char* tile, int tr_off,
 __device__ __forceinline__ void copy_floats(const float* base, unsigned off, unsigned lds_addr) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, %0" : : "s"(base), "v"(off), "s"(lds_addr) : "memory", "m0");
 }
-// Waits for all but KEEP of this wavefront's copies and for its LDS reads, then meets the workgroup's other wavefronts.
-template <int KEEP>
+// Waits for all but COUNT of this wavefront's copies and for its LDS reads, then meets the workgroup's other wavefronts.
+// (SLA_FULL_WAITS: a checking build that waits for all of them, whose results have to be the same bits.)
+template <int COUNT>
 __device__ __forceinline__ void copies_barrier() {
-  static_assert(KEEP < 64, "the counter's range");
+  static_assert(COUNT < 64, "the counter's range");
+#ifdef SLA_FULL_WAITS
+  constexpr int KEEP = 0;
+#else
+  constexpr int KEEP = COUNT;
+#endif
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0x0070 | (KEEP & 15) | ((KEEP >> 4) << 14));  // vmcnt(KEEP) lgkmcnt(0)
   __builtin_amdgcn_s_barrier();

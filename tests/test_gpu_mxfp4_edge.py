@@ -84,3 +84,21 @@ def test_every_exponent_of_activations_with_every_one_of_weights(M, N, K):
     # far below fp32's range nothing is left, far above it no finite number
     assert (np.abs(y[size < 1e-46]) == 0).all()
     assert not np.isfinite(y[np.abs(want) > 1e39]).any()
+
+
+@pytest.mark.parametrize("M,N,K", KERNELS + [(1100, 1304, 1800), (3000, 1800, 520), (2100, 2184, 136), (2300, 2056, 1536), (33000, 520, 520), (65600, 1032, 1024), (66000, 776, 1280), (20000, 5128, 2568)])
+def test_counted_copy_waits_agree_with_full_waits(M, N, K):
+    """The kernels of the larger products wait for their copies by hand-counted `vmcnt` values; a second build of the library
+    (-DSLA_FULL_WAITS) waits for every copy each time.  The two agree bit for bit, in calls that follow one another at once."""
+    import ctypes
+    import os
+    from paper_2512_16093_amd import build
+    assert os.path.exists(build.LIB_FULL_WAITS), "run python -m paper_2512_16093_amd.build"
+    full = ctypes.CDLL(build.LIB_FULL_WAITS).mxfp4_gemm_fwd
+    full.restype, full.argtypes = ctypes.c_int, sla.lib().mxfp4_gemm_fwd.argtypes
+    xq, wq, bias = sla.mxfp4_quantize(_bf16(M, (M, K))), sla.mxfp4_quantize(_bf16(N, (N, K), K ** -0.5)), _bf16(K, N)
+    got = [sla.mxfp4_gemm_fwd(xq, wq, M, N, K, bias=bias) for _ in range(3)]
+    want = torch.empty_like(got[0])
+    assert full(xq.data_ptr(), xq.numel(), wq.data_ptr(), wq.numel(), bias.data_ptr(), want.data_ptr(), M, N, K,
+                torch.cuda.current_stream().cuda_stream) == 0
+    assert all(torch.equal(y, want) for y in got)
