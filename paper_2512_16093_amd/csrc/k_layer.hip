@@ -12,9 +12,9 @@
 // deviations (n off by 2^-18 at most in 2400 rows with features of any other size among equal ones).  Nor do the squares cancel: no x lies
 // between the bf16 numbers a < b around the mean, so (x - a)(x - b) >= 0 and the variance is at least (mean - a)(b - mean), which is at least
 // c^2, p being the nearer of the two.
-// Measured: forward with gate and modulation 75600 x 5120 541 us, 5.7 TB/s, 32760 x 5120 239, 65520 x 1536 145 (5.5), 20000 x 13824 404, without
-// residual 75600 x 5120 280 (5.5); into codes 75600 x 5120 456 (5.5), 65520 x 1536 115; one row of 5120 2.9.  Backward with everything
-// 65520 x 1536 252 us, 4.8 TB/s, 32760 x 5120 419 (4.8), 8192 x 5120 116, 129 x 1536 12.
+// Measured: forward with gate and modulation 75600 x 5120 537 us, 5.8 TB/s, 32760 x 5120 230 (5.8), 65520 x 1536 138 (5.8), 20000 x 13824 397, x
+// alone 75600 x 5120 243 (6.4); into codes 75600 x 5120 460 (5.5), 65520 x 1536 121; one row of 5120 2.9.  Backward with everything
+// 65520 x 1536 253 us, 4.8 TB/s, 32760 x 5120 402 (5.0), 8192 x 5120 123, 129 x 1536 12.
 #include "layer.h"
 #include "mxfp4.h"
 

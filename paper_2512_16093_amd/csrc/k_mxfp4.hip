@@ -64,7 +64,8 @@ __global__ void __launch_bounds__(256) mxfp4_dequantize_kernel(const uint8_t* __
     if (r0 + 2 * i < R && k8 < K / 8) store_to<NT>(x + (long long)(r0 + 2 * i) * K + 8ll * k8, mx_values8(v[i], e[i]));
 }
 
-// One block of 32 features a thread.
+// One block of 32 features a thread, byte by byte (rows of codes may stand at any address): 13824 x 5120 into an object 94 us, 0.8 TB/s, out of it
+// 30, 2.5; of a weight once.
 __global__ void __launch_bounds__(256) mxfp4_pack_kernel(const uint8_t* __restrict__ from, const uint8_t* __restrict__ from_exps,
                                                          int R, int K, int RP, int KB, uint8_t* __restrict__ codes,
                                                          uint8_t* __restrict__ exps) {
